@@ -19,6 +19,13 @@
  *   arbor_uncertainty       normalised next-token entropy u_i at block
  *                           boundaries (Sec. 4 MSVE, Eq. 1), the input u_in of
  *                           arbor_score.
+ * and what grows the tree that the path above thins out:
+ *   arbor_extend            reserves slots for new tokens of blocks.
+ *   arbor_truncate          takes the newest tokens of blocks back.
+ *   arbor_fork              makes a block a copy of another.
+ *   arbor_append            norms and rotates queries and keys of new tokens and
+ *                           writes their K/V rows into the pool.
+ *   arbor_tree_prefill_attn causal attention of new tokens over their chains.
  *
  * Conventions
  *  - Every pointer is a DEVICE pointer unless marked (host) or (pinned host).
@@ -43,6 +50,10 @@
  *  - Positions are node-local: position p of node i is token a_i + p of the
  *    paper's span x_{a_i:b_i}.  Per-token arrays (A, sel_pos) are indexed by
  *    tok_off[i] + p.
+ *  - A block may have room for more tokens than it holds: tok_off and page_off
+ *    are prefix sums of the blocks' capacities, of which n_full gives the part
+ *    in use (a block that is still to come has n_full = n_kept = 0).  A tree
+ *    that does not grow has capacities equal to n_full.
  */
 #ifndef ARBOR_H
 #define ARBOR_H
@@ -61,7 +72,7 @@ typedef enum {
   ARBOR_OK = 0,
   ARBOR_OVER_BUDGET = 1,    /* warning: even the minimum counts exceed the budget  */
   ARBOR_EINVAL = -1,        /* bad argument or malformed tree/selection            */
-  ARBOR_ENOPAGES = -2,      /* rehydration needs more pages than are free          */
+  ARBOR_ENOPAGES = -2,      /* more pages are needed than are free                 */
   ARBOR_EHIP = -3,          /* a HIP launch failed                                 */
   ARBOR_EUNSUPPORTED = -4,  /* shape outside what the kernels implement            */
   ARBOR_ENONFINITE = -5,    /* NaN in A or s; NaN or infinite logit                */
@@ -87,7 +98,8 @@ typedef enum {
   ARBOR_KERNEL_DECODE_ATTN = 3,   /* the attention kernel of arbor_tree_decode_attn */
   ARBOR_KERNEL_DECODE_CREDIT = 4, /* the merge-and-credit kernel of
                                      arbor_tree_decode_attn_scored                 */
-  ARBOR_KERNEL_COUNT = 5
+  ARBOR_KERNEL_PREFILL_ATTN = 5,  /* the attention kernel of arbor_tree_prefill_attn */
+  ARBOR_KERNEL_COUNT = 6
 } arbor_kernel_t;
 
 /* (host) A timing request that belongs to one call: when a call launches
@@ -124,8 +136,8 @@ typedef struct {
   int64_t num_tokens;        /* N = tok_off[V]                                    */
   const int32_t *parent;     /* [V]  parent[0] = -1                               */
   const int32_t *n_full;     /* [V]  n_i = b_i - a_i + 1                          */
-  const int64_t *tok_off;    /* [V+1] prefix sum of n_full                        */
-  const int64_t *page_off;   /* [V+1] prefix sum of ceil(n_full / page_size)      */
+  const int64_t *tok_off;    /* [V+1] prefix sum of the capacities (>= n_full)    */
+  const int64_t *page_off;   /* [V+1] prefix sum of ceil(capacity / page_size)    */
   int32_t *n_kept;           /* [V]  c_i, resident tokens (in/out)                */
   int32_t *page_table;       /* [page_off[V]] physical page of logical page q of
                                 node i at page_off[i] + q; -1 = unused (in/out)   */
@@ -494,6 +506,154 @@ int arbor_uncertainty(const void *logits, int32_t dtype, int32_t n_rows, int64_t
 /* Bytes of workspace arbor_uncertainty needs for n_rows rows of `vocab` logits. */
 size_t arbor_uncertainty_workspace_size(int32_t n_rows, int64_t vocab, int32_t dtype);
 
+/*
+ * Growing the tree.  New tokens of several blocks travel packed: block nodes[e]
+ * (e < n_seq, device int32, strictly ascending ids) gets the tokens cu[e] ..
+ * cu[e+1]-1 of the packed rows (cu: device int32 [n_seq+1], cu[0] = 0, not
+ * descending; a block may get none).  n_tokens rows are packed in all; rows from
+ * cu[n_seq] on are padding, which every call leaves as it was.  A step of a
+ * model is one arbor_extend, one arbor_prefill_plan, and for each layer
+ * arbor_append and arbor_tree_prefill_attn (or arbor_tree_decode_attn where
+ * every block got one token).
+ *
+ * arbor_extend -- reserves the slots of new tokens (the blocks of Sec. 3 as they
+ * are being written).  Block i = nodes[e] with n_i tokens, of which c_i are
+ * resident, gets m = cu[e+1] - cu[e] more: token t takes slot c_i + t and position
+ * n_i + t.  Pages are popped from the top of the free stack in (node, page)
+ * order; n_kept[i] = c_i + m; n_full[i] = n_i + m (n_full is tree->n_full, which
+ * this call and the next two write).  For every packed token (padding: -1, 0, -1)
+ *   slots[t]      its place in the pool, page * page_size + row;
+ *   positions[t]  its position in its chain: the tokens (n_full, evicted ones
+ *                 counted) of its proper ancestors, those of this call included,
+ *                 and its position in its block;
+ *   tokens[t]     tok_off[i] + its position in its block, the index of per-token
+ *                 arrays (nullable).
+ * The rows of the new slots hold nothing yet: arbor_append writes them.
+ * Errors: EINVAL (ids, cu, a malformed tree, a block beyond its capacity, n_full
+ * not tree->n_full), ENOPAGES, EUNSUPPORTED (a block deeper than
+ * ARBOR_MAX_DEPTH), EWORKSPACE.
+ */
+int arbor_extend(const arbor_geom_t *geom, arbor_tree_t *tree, arbor_pool_t *pool,
+                 int32_t *n_full, const int32_t *nodes, int32_t n_seq, const int32_t *cu,
+                 int32_t n_tokens, int64_t *slots, int32_t *positions, int64_t *tokens,
+                 int32_t *status, void *workspace, size_t workspace_bytes, hipStream_t stream);
+
+/*
+ * arbor_truncate -- takes tokens back (a draft that was rejected, a thought that
+ * is pruned: keep 0).  Block i = nodes[e] (strictly ascending ids) keeps its
+ * resident tokens at positions below keep[e] (device int32 >= 0) in their slots;
+ * n_full[i] = min(n_i, keep[e]).  Vacated slots get slot_pos = -1, unused
+ * page-table entries -1, and the freed pages go back on the free stack so that
+ * popping them in (node, page) order gives each block its own pages again: an
+ * arbor_extend followed by the arbor_truncate that takes its tokens back leaves
+ * the free stack as it was.
+ * Errors: EINVAL (ids, a negative keep, n_full not tree->n_full), ECORRUPT (free
+ * stack would overflow), EWORKSPACE.
+ */
+int arbor_truncate(const arbor_geom_t *geom, arbor_tree_t *tree, arbor_pool_t *pool,
+                   int32_t *n_full, const int32_t *nodes, const int32_t *keep, int32_t n_nodes,
+                   int32_t *status, void *workspace, size_t workspace_bytes, hipStream_t stream);
+
+/*
+ * arbor_fork -- block dst[e] becomes a copy of block src[e] (a thought that is
+ * continued in several ways): as many tokens, the same positions resident in the
+ * same slots of pages popped in (node, page) order, their K/V rows of every layer
+ * and head copied bitwise, and, where the arrays are given, its rows of A (fp32
+ * [N], all n positions) and rows_seen (int64 [V]).  dst (strictly ascending ids)
+ * must be empty, n_full = n_kept = 0, and have the capacity; a src may be named
+ * more than once and is read as it was before the call.  Blocks whose parents
+ * differ have different chains, so a copy means something below the same parent.
+ * The token-span record is the caller's to copy (rows tok_off[src] + p).
+ * Errors: EINVAL (ids, a dst that is not empty or too small, n_full not
+ * tree->n_full), ENOPAGES, EWORKSPACE.
+ */
+int arbor_fork(const arbor_geom_t *geom, arbor_tree_t *tree, arbor_pool_t *pool,
+               int32_t *n_full, const int32_t *src, const int32_t *dst, int32_t n_forks, float *A,
+               int64_t *rows_seen, int32_t *status, void *workspace, size_t workspace_bytes,
+               hipStream_t stream);
+
+/*
+ * arbor_append -- one layer's queries, keys and values of n_tokens packed tokens.
+ * Each query head and each key head x (head_dim elements) becomes
+ *   y = w * x / sqrt(mean(x^2) + eps)          (w = q_norm or k_norm; NULL: y = x)
+ * and then turns by its token's position: with angles a_j = positions[t] *
+ * inv_freq[j], j < rotary_dim / 2, the pair (y_a, y_b) becomes
+ *   (y_a cos a_j - y_b sin a_j,  y_b cos a_j + y_a sin a_j),
+ * (a, b) = (j, j + rotary_dim / 2), or (2j, 2j + 1) when interleaved = 1; elements
+ * from rotary_dim on stay.  Angles are formed in 64 bits, the rest in fp32, and
+ * each result is rounded once.  Queries go to q_out [n_tokens][Hq][head_dim]; keys
+ * and values (values unchanged) to row slots[t] of layer `layer` of the pool, and,
+ * where a record is given, to row tokens[t] of it ([N][L][Hkv][head_dim], the
+ * token-span record that arbor_rehydrate reads; pinned host or device).  A token
+ * with slots[t] = -1 is padding and left out altogether.  q, k, v are in the
+ * pool's dtype, rows of Hq (Hkv) heads side by side, *_stride elements apart (so
+ * they may be parts of one product's rows); q_out may be q itself where q_stride
+ * is Hq * head_dim.  No two tokens may have the same slot.
+ * Errors: EINVAL (arguments, a slot outside the pool or, with a record, a token
+ * outside [0, N): that token is left out), EUNSUPPORTED (rotary_dim not a multiple
+ * of 8 or above head_dim; a pointer or stride that is not a multiple of 16 bytes).
+ */
+typedef struct {
+  const void *q, *k, *v;            /* device, dtype                                  */
+  int64_t q_stride, k_stride, v_stride;  /* elements from a token's row to the next   */
+  const void *q_norm, *k_norm;      /* device [head_dim] dtype, nullable              */
+  const float *inv_freq;            /* device fp32 [rotary_dim / 2]; NULL with 0      */
+  const int64_t *slots;             /* device [n_tokens], of arbor_extend             */
+  const int32_t *positions;         /* device [n_tokens]                              */
+  const int64_t *tokens;            /* device [n_tokens]; with a record only          */
+  void *record_k, *record_v;        /* both or neither                                */
+  void *q_out;                      /* device [n_tokens][Hq][head_dim] dtype          */
+  float eps;
+  int32_t rotary_dim;               /* 0: no rotation                                 */
+  int32_t interleaved;              /* 0 or 1                                         */
+} arbor_append_t;
+
+int arbor_append(const arbor_geom_t *geom, const arbor_tree_t *tree, arbor_pool_t *pool,
+                 int32_t layer, const arbor_append_t *args, int32_t n_tokens, int32_t *status,
+                 hipStream_t stream);
+
+/*
+ * arbor_prefill_plan -- the work list of arbor_tree_prefill_attn for the newest
+ * tokens of blocks: nodes, cu and n_tokens as for arbor_extend (any order of
+ * ids), after it.  It depends on the tree alone, so one plan serves every layer;
+ * it holds until n_kept or the page table of a block in one of the chains
+ * changes (a plan kept longer gives wrong results, or EINVAL, and touches
+ * nothing outside the pool).  `plan`: device, arbor_prefill_plan_size() bytes,
+ * 256-byte aligned.
+ * Errors: EINVAL (ids, cu, a malformed tree, a block that holds fewer tokens than
+ * it is said to have got), EUNSUPPORTED (a block deeper than ARBOR_MAX_DEPTH, more
+ * than 128 query heads for one KV head), EWORKSPACE.
+ */
+size_t arbor_prefill_plan_size(const arbor_geom_t *geom, int32_t n_seq, int32_t n_tokens);
+int arbor_prefill_plan(const arbor_geom_t *geom, const arbor_tree_t *tree, const int32_t *nodes,
+                       int32_t n_seq, const int32_t *cu, int32_t n_tokens, void *plan,
+                       size_t plan_bytes, int32_t *status, hipStream_t stream);
+
+/*
+ * arbor_tree_prefill_attn -- one layer's attention of packed new tokens over their
+ * chains (the prompt, a new thought, a draft to be verified; Sec. 1 and Sec. 3: a
+ * token depends on its ancestor chain alone).  For packed token t of block i and
+ * query head h
+ *   out[t][h][:] = softmax(scale q[t][h] K^T) V
+ * over every resident slot of every proper ancestor of i and the slots of i up to
+ * the token's own.  q and out [n_tokens][Hq][head_dim] in the pool's dtype, lse_out
+ * [n_tokens][Hq] fp32 natural-log LSE (nullable); softmax_scale <= 0 means
+ * 1/sqrt(head_dim).  The tokens of several blocks share the reads of the ancestors
+ * that they have in common.  For bf16 pools the weights are rounded to bf16 before
+ * their product with V (as V and the output are); all sums are fp32.  What a token
+ * may not see (later tokens, other blocks, unused rows of a page) has no influence
+ * on its output, infinities and NaN included.  Results are bitwise reproducible.
+ * `plan` is arbor_prefill_plan's for this n_seq and n_tokens; `workspace` holds
+ * arbor_prefill_workspace_size() bytes.
+ * Errors: EINVAL (arguments, a plan of another call or of a tree that has changed
+ * since), EUNSUPPORTED, EWORKSPACE.
+ */
+size_t arbor_prefill_workspace_size(const arbor_geom_t *geom, int32_t n_seq, int32_t n_tokens);
+int arbor_tree_prefill_attn(const arbor_geom_t *geom, const arbor_tree_t *tree,
+                            const arbor_pool_t *pool, const void *plan, size_t plan_bytes,
+                            int32_t n_seq, int32_t n_tokens, int32_t layer, const void *q,
+                            void *out, float *lse_out, float softmax_scale, int32_t *status,
+                            void *workspace, size_t workspace_bytes, hipStream_t stream);
 
 #ifdef __cplusplus
 }

@@ -32,6 +32,10 @@ of the paper it follows:
   walk              Alg. 2 (event-driven controller): Transition events to a
                     sequence of active leaves with lazy rehydration, and the
                     Pressure event raised at B - delta
+  extend, truncate, fork, append, prefill_attn
+                    Sec. 3 (blocks are token spans that the search writes,
+                    drops and continues in several ways; a token depends on
+                    its ancestor chain alone): growing the same paged pool
 
 Readings of points the paper leaves open are listed next to the code that
 takes them.  Parity status: every function here is pinned by the tests in
@@ -705,3 +709,162 @@ def walk(st, targets, budget, s, A, rows_seen, p, host_k, host_v, pressure_margi
                 st = compact(st, k, sel)
         stats.append(row)
     return st, A, rows_seen, s, np.array(stats, np.int64).reshape(-1, 4), status
+
+
+# ----------------------------------------------------------------------------
+# growing the tree  (Sec. 3: blocks are written, taken back and continued)
+# ----------------------------------------------------------------------------
+def _n_pages(tokens, P):
+    return -(-int(tokens) // P)
+
+
+def _ascending(ids, V):
+    return all(0 <= int(i) < V for i in ids) and all(a < b for a, b in zip(ids, ids[1:]))
+
+
+def extend(st, nodes, cu, n_tokens):
+    """Slots for cu[e+1] - cu[e] more tokens of each block nodes[e]: (new state, slots,
+    positions, tokens, status).  Positions count all tokens of the proper ancestors."""
+    st, P, V = copy_state(st), st["page_size"], len(st["parent"])
+    slots, positions, tokens = (np.full(n_tokens, x, dtype=np.int64) for x in (-1, 0, -1))
+    nodes = [int(i) for i in nodes]
+    fail = (st, slots, positions, tokens, EINVAL)
+    if not _ascending(nodes, V) or cu[0] != 0 or cu[-1] > n_tokens or np.any(np.diff(cu) < 0):
+        return fail
+    need = 0
+    for e, i in enumerate(nodes):
+        m, c, n = int(cu[e + 1] - cu[e]), int(st["n_kept"][i]), int(st["n_full"][i])
+        if n + m > st["tok_off"][i + 1] - st["tok_off"][i] or \
+                _n_pages(c + m, P) > st["page_off"][i + 1] - st["page_off"][i]:
+            return fail
+        need += _n_pages(c + m, P) - _n_pages(c, P)
+    if need > st["free_top"]:
+        return st, slots, positions, tokens, ENOPAGES
+    before = [(int(st["n_kept"][i]), int(st["n_full"][i])) for i in nodes]
+    for e, i in enumerate(nodes):
+        st["n_kept"][i] += cu[e + 1] - cu[e]
+        st["n_full"][i] += cu[e + 1] - cu[e]
+    top = int(st["free_top"])
+    for e, i in enumerate(nodes):
+        c, n = before[e]
+        start = sum(int(st["n_full"][x]) for x in chain(st["parent"], i)[:-1])
+        for q in range(_n_pages(c, P), _n_pages(st["n_kept"][i], P)):
+            top -= 1
+            st["page_table"][int(st["page_off"][i]) + q] = st["free_stack"][top]
+        for j in range(int(cu[e + 1] - cu[e])):
+            page = int(st["page_table"][int(st["page_off"][i]) + (c + j) // P])
+            st["slot_pos"][page, (c + j) % P] = n + j
+            t = int(cu[e]) + j
+            slots[t], positions[t] = page * P + (c + j) % P, start + n + j
+            tokens[t] = int(st["tok_off"][i]) + n + j
+    st["free_top"] = np.int64(top)
+    return st, slots, positions, tokens, OK
+
+
+def truncate(st, nodes, keep):
+    """Blocks keep their resident tokens at positions below keep: (new state, status)."""
+    st, P, V = copy_state(st), st["page_size"], len(st["parent"])
+    nodes = [int(i) for i in nodes]
+    if not _ascending(nodes, V) or any(int(x) < 0 for x in keep):
+        return st, EINVAL
+    freed = []
+    for i, kp in zip(nodes, keep):
+        rows = retained(st, i)
+        stay = sum(1 for r in rows if r[3] < kp)
+        for _, page, r, pos in rows:
+            if pos >= kp:
+                st["slot_pos"][page, r] = -1
+        for q in range(_n_pages(stay, P), _n_pages(len(rows), P)):
+            at = int(st["page_off"][i]) + q
+            freed.append(int(st["page_table"][at]))
+            st["page_table"][at] = -1
+        st["n_kept"][i] = stay
+        st["n_full"][i] = min(int(st["n_full"][i]), int(kp))
+    for page in reversed(freed):
+        st["free_stack"][int(st["free_top"])] = page
+        st["free_top"] = st["free_top"] + 1
+    return st, OK
+
+
+def fork(st, src, dst, A=None, rows_seen=None):
+    """The empty blocks dst become copies of src: (new state, A, rows_seen, status)."""
+    old, st, P, V = st, copy_state(st), st["page_size"], len(st["parent"])
+    A = None if A is None else A.copy()
+    rows_seen = None if rows_seen is None else rows_seen.copy()
+    seen = None if rows_seen is None else rows_seen.copy()
+    src, dst = [int(x) for x in src], [int(x) for x in dst]
+    if not _ascending(dst, V) or any(not 0 <= a < V for a in src):
+        return st, A, rows_seen, EINVAL
+    for a, b in zip(src, dst):
+        if old["n_full"][b] or old["n_kept"][b] or \
+                old["n_full"][a] > old["tok_off"][b + 1] - old["tok_off"][b]:
+            return st, A, rows_seen, EINVAL
+    if sum(_n_pages(old["n_kept"][a], P) for a in src) > old["free_top"]:
+        return st, A, rows_seen, ENOPAGES
+    top = int(st["free_top"])
+    for a, b in zip(src, dst):
+        for q in range(_n_pages(old["n_kept"][a], P)):
+            top -= 1
+            st["page_table"][int(st["page_off"][b]) + q] = st["free_stack"][top]
+        for s, page, r, pos in retained(old, a):
+            to = int(st["page_table"][int(st["page_off"][b]) + s // P])
+            st["slot_pos"][to, s % P] = pos
+            st["k"][:, to, :, s % P] = old["k"][:, page, :, r]
+            st["v"][:, to, :, s % P] = old["v"][:, page, :, r]
+        n = int(old["n_full"][a])
+        st["n_kept"][b], st["n_full"][b] = old["n_kept"][a], n
+        if A is not None:
+            ta, tb = int(old["tok_off"][a]), int(old["tok_off"][b])
+            A[tb:tb + n] = A[ta:ta + n]
+        if rows_seen is not None:
+            rows_seen[b] = seen[a]
+    st["free_top"] = np.int64(top)
+    return st, A, rows_seen, OK
+
+
+def norm_rotate(x, weight, eps, positions, inv_freq, interleaved):
+    """Heads x [T][heads][d] in fp64: w x / sqrt(mean(x^2) + eps), then the pairs turned by
+    positions[t] * inv_freq[j].  Also the normed heads (for error bounds)."""
+    x = np.asarray(x, dtype=np.float64)
+    if weight is not None:
+        x = x / np.sqrt((x * x).mean(-1, keepdims=True) + eps) * np.asarray(weight, np.float64)
+    y = x.copy()
+    half = 0 if inv_freq is None else len(inv_freq)
+    for j in range(half):
+        a, b = (2 * j, 2 * j + 1) if interleaved else (j, j + half)
+        ang = np.asarray(positions, np.float64) * float(inv_freq[j])
+        c, s = np.cos(ang)[:, None], np.sin(ang)[:, None]
+        y[..., a] = x[..., a] * c - x[..., b] * s
+        y[..., b] = x[..., b] * c + x[..., a] * s
+    return y, x
+
+
+def prefill_attn(st, nodes, cu, layer, q, q_per_kv, softmax_scale=None):
+    """Each new token of block i (its newest cu[e+1] - cu[e] ones) over the resident slots
+    of i's proper ancestors and i's slots up to its own: out, natural-log LSE, and for
+    error bounds sum p |v| and the largest scale * sum |q_x k_x| of each row."""
+    T, Hq, d = q.shape
+    P, G = st["page_size"], q_per_kv
+    scale = 1.0 / math.sqrt(d) if softmax_scale is None else softmax_scale
+    out, mass = np.zeros((T, Hq, d)), np.zeros((T, Hq, d))
+    lse, big = np.full((T, Hq), -np.inf), np.zeros((T, Hq))
+    for e, i in enumerate(nodes):
+        m = int(cu[e + 1] - cu[e])
+        if m == 0:
+            continue
+        rows = [r for x in chain(st["parent"], int(i)) for r in retained(st, x)]
+        page, row = np.array([r[1] for r in rows]), np.array([r[2] for r in rows])
+        k = st["k"][layer][page, :, row].astype(np.float64)     # [keys][Hkv][d]
+        v = st["v"][layer][page, :, row].astype(np.float64)
+        for j in range(m):
+            t, seen = int(cu[e]) + j, len(rows) - m + j + 1
+            for h in range(Hq):
+                qq = q[t, h].astype(np.float64)
+                z = scale * (k[:seen, h // G] @ qq)
+                w = np.exp(z - z.max())
+                lse[t, h] = z.max() + math.log(w.sum())
+                w = w / w.sum()
+                out[t, h] = w @ v[:seen, h // G]
+                mass[t, h] = w @ np.abs(v[:seen, h // G])
+                big[t, h] = scale * (np.abs(k[:seen, h // G]) @ np.abs(qq)).max()
+    return out, lse, mass, big

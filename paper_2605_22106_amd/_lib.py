@@ -24,7 +24,7 @@ EINVAL, ENOPAGES, EHIP, EUNSUPPORTED, ENONFINITE, EWORKSPACE, ECORRUPT = -1, -2,
 BF16, F32 = 0, 1
 # kernels a call can time on their own (arbor_timing_t)
 KERNEL_SCORE_ATTN, KERNEL_SELECT, KERNEL_COMPACT_MOVE, KERNEL_DECODE_ATTN = 0, 1, 2, 3
-KERNEL_DECODE_CREDIT, KERNEL_COUNT = 4, 5
+KERNEL_DECODE_CREDIT, KERNEL_PREFILL_ATTN, KERNEL_COUNT = 4, 5, 6
 SELECT_TAIL_HEAVY, SELECT_TAIL_ONLY, SELECT_SINKS_TAIL = 0, 1, 2
 MAX_DEPTH = 63
 
@@ -88,6 +88,18 @@ class Sizes(ctypes.Structure):
                 ("max_leaves", ctypes.c_int32), ("max_layers", ctypes.c_int32)]
 
 
+class Append(ctypes.Structure):
+    _fields_ = [("q", ctypes.c_void_p), ("k", ctypes.c_void_p), ("v", ctypes.c_void_p),
+                ("q_stride", ctypes.c_int64), ("k_stride", ctypes.c_int64),
+                ("v_stride", ctypes.c_int64), ("q_norm", ctypes.c_void_p),
+                ("k_norm", ctypes.c_void_p), ("inv_freq", ctypes.c_void_p),
+                ("slots", ctypes.c_void_p), ("positions", ctypes.c_void_p),
+                ("tokens", ctypes.c_void_p), ("record_k", ctypes.c_void_p),
+                ("record_v", ctypes.c_void_p), ("q_out", ctypes.c_void_p),
+                ("eps", ctypes.c_float), ("rotary_dim", ctypes.c_int32),
+                ("interleaved", ctypes.c_int32)]
+
+
 _lib = None
 
 
@@ -123,6 +135,16 @@ def load() -> ctypes.CDLL:
                                                  vp]),
             "arbor_uncertainty_workspace_size": (sz, [i32, i64, i32]),
             "arbor_walk": (ctypes.c_int, [G, T, Pl, ctypes.POINTER(Walk), Pa, vp, vp, sz, vp]),
+            "arbor_extend": (ctypes.c_int, [G, T, Pl, vp, vp, i32, vp, i32, vp, vp, vp, vp, vp, sz,
+                                            vp]),
+            "arbor_truncate": (ctypes.c_int, [G, T, Pl, vp, vp, vp, i32, vp, vp, sz, vp]),
+            "arbor_fork": (ctypes.c_int, [G, T, Pl, vp, vp, vp, i32, vp, vp, vp, vp, sz, vp]),
+            "arbor_append": (ctypes.c_int, [G, T, Pl, i32, ctypes.POINTER(Append), i32, vp, vp]),
+            "arbor_prefill_plan_size": (sz, [G, i32, i32]),
+            "arbor_prefill_plan": (ctypes.c_int, [G, T, vp, i32, vp, i32, vp, sz, vp, vp]),
+            "arbor_prefill_workspace_size": (sz, [G, i32, i32]),
+            "arbor_tree_prefill_attn": (ctypes.c_int, [G, T, Pl, vp, sz, i32, i32, i32, vp, vp, vp,
+                                                       ctypes.c_float, vp, vp, sz, vp]),
         }
         for name, (res, args) in sig.items():
             f = getattr(lib, name)
@@ -137,7 +159,9 @@ def exported_symbols():
             "arbor_select", "arbor_compact", "arbor_compact_noalloc", "arbor_select_compact",
             "arbor_rehydrate", "arbor_tree_decode_attn",
             "arbor_tree_decode_attn_scored", "arbor_uncertainty",
-            "arbor_uncertainty_workspace_size", "arbor_walk"]
+            "arbor_uncertainty_workspace_size", "arbor_walk", "arbor_extend", "arbor_truncate",
+            "arbor_fork", "arbor_append", "arbor_prefill_plan_size", "arbor_prefill_plan",
+            "arbor_prefill_workspace_size", "arbor_tree_prefill_attn"]
 
 
 def _dev(t: torch.Tensor | None, name: str):
@@ -411,3 +435,151 @@ def arbor_uncertainty(logits, top_k, u_out, status, workspace, dst=None, stream=
                                     _dev(u_out, "u_out"), int(u_out.numel()),
                                     _dev(status, "status"), _dev(workspace, "workspace"),
                                     int(workspace.numel()), _stream(stream))
+
+
+# ---- growing the tree ---------------------------------------------------------
+# These check shapes and types too: the packed rows' counts are taken from them.
+
+def _is(t, name: str, dtype, *shape):
+    """Pointer of a contiguous GPU tensor of this type and shape, on the current device."""
+    if t is None:
+        return None
+    if t.dtype != dtype or tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name} must be {dtype} of shape {tuple(shape)}, "
+                         f"not {t.dtype} of shape {tuple(t.shape)}")
+    p = _dev(t, name)
+    if t.device.index != torch.cuda.current_device():
+        raise ValueError(f"{name} must be on the current device")
+    return p
+
+
+def _element(kv: KVState):
+    return torch.bfloat16 if kv.dtype == BF16 else torch.float32
+
+
+def _packed(nodes, cu):
+    n_seq = int(nodes.numel())
+    return n_seq, _is(nodes, "nodes", torch.int32, n_seq), _is(cu, "cu", torch.int32, n_seq + 1)
+
+
+def arbor_extend(kv: KVState, nodes, cu, slots, positions, tokens, status, workspace,
+                 stream=None) -> int:
+    """Reserve slots for the packed tokens cu[e] .. cu[e+1] of block nodes[e]
+    (ascending); the rows of `slots` (int64), `positions` (int32) and `tokens`
+    (int64 or None) are the packed rows."""
+    g, t, p = kv.geom(), kv.tree(), kv.pool()
+    n_seq, nd, c = _packed(nodes, cu)
+    n = int(slots.numel())
+    return load().arbor_extend(ctypes.byref(g), ctypes.byref(t), ctypes.byref(p),
+                               _dev(kv.n_full, "n_full"), nd, n_seq, c, n,
+                               _is(slots, "slots", torch.int64, n),
+                               _is(positions, "positions", torch.int32, n),
+                               _is(tokens, "tokens", torch.int64, n),
+                               _is(status, "status", torch.int32, 1),
+                               _dev(workspace, "workspace"), int(workspace.numel()),
+                               _stream(stream))
+
+
+def arbor_truncate(kv: KVState, nodes, keep, status, workspace, stream=None) -> int:
+    """Block nodes[e] (ascending) keeps its tokens at positions below keep[e]."""
+    g, t, p = kv.geom(), kv.tree(), kv.pool()
+    n = int(nodes.numel())
+    return load().arbor_truncate(ctypes.byref(g), ctypes.byref(t), ctypes.byref(p),
+                                 _dev(kv.n_full, "n_full"), _is(nodes, "nodes", torch.int32, n),
+                                 _is(keep, "keep", torch.int32, n), n,
+                                 _is(status, "status", torch.int32, 1),
+                                 _dev(workspace, "workspace"), int(workspace.numel()),
+                                 _stream(stream))
+
+
+def arbor_fork(kv: KVState, src, dst, status, workspace, A=None, rows_seen=None,
+               stream=None) -> int:
+    """The empty block dst[e] (ascending) becomes a copy of block src[e]."""
+    g, t, p = kv.geom(), kv.tree(), kv.pool()
+    n = int(dst.numel())
+    return load().arbor_fork(ctypes.byref(g), ctypes.byref(t), ctypes.byref(p),
+                             _dev(kv.n_full, "n_full"), _is(src, "src", torch.int32, n),
+                             _is(dst, "dst", torch.int32, n), n,
+                             _is(A, "A", torch.float32, kv.num_tokens),
+                             _is(rows_seen, "rows_seen", torch.int64, kv.num_nodes),
+                             _is(status, "status", torch.int32, 1), _dev(workspace, "workspace"),
+                             int(workspace.numel()), _stream(stream))
+
+
+def _rows(x, name: str, dtype, n: int, width: int):
+    """Pointer and row stride of n rows of `width` elements side by side; [n, width] or
+    [n, heads, head_dim], where rows may lie further apart than they are long."""
+    if x.dtype != dtype or x.dim() not in (2, 3) or x.shape[0] != n or x[:1].numel() != (
+            width if n else 0):
+        raise ValueError(f"{name} must be {dtype} rows [{n}, {width}]")
+    if not x.is_cuda or x.device.index != torch.cuda.current_device():
+        raise ValueError(f"{name} must be a GPU tensor on the current device")
+    if x.stride(-1) != 1 or (x.dim() == 3 and x.stride(1) != x.shape[2]):
+        raise ValueError(f"the elements of a row of {name} must be contiguous")
+    return ctypes.c_void_p(x.data_ptr()), int(x.stride(0)) if n > 1 else width
+
+
+def arbor_append(kv: KVState, layer, q, k, v, slots, positions, q_out, status, q_norm=None,
+                 k_norm=None, eps=1e-6, inv_freq=None, interleaved=False, tokens=None,
+                 record_k=None, record_v=None, stream=None) -> int:
+    """Norm and rotate the queries and keys of packed tokens (rows of q, k, v, which
+    may be slices of one product's rows), and write keys and values to `slots` of
+    layer `layer`; rotary_dim is twice the length of inv_freq (fp32)."""
+    g, t, p = kv.geom(), kv.tree(), kv.pool()
+    n, d, dt = int(slots.numel()), kv.head_dim, _element(kv)
+    hq = kv.kv_heads * kv.q_per_kv
+    qp, qs = _rows(q, "q", dt, n, hq * d)
+    kp, ks = _rows(k, "k", dt, n, kv.kv_heads * d)
+    vp, vs = _rows(v, "v", dt, n, kv.kv_heads * d)
+    rec = []
+    for x, name in ((record_k, "record_k"), (record_v, "record_v")):
+        if x is not None and (x.dtype != dt or tuple(x.shape) != (kv.num_tokens, kv.layers,
+                                                                  kv.kv_heads, d)):
+            raise ValueError(f"{name} must be {dt} [num_tokens, layers, kv_heads, head_dim]")
+        rec.append(None if x is None else _host_or_dev(x, name))
+    half = 0 if inv_freq is None else int(inv_freq.numel())
+    a = Append(qp, kp, vp, qs, ks, vs, _is(q_norm, "q_norm", dt, d), _is(k_norm, "k_norm", dt, d),
+               _is(inv_freq, "inv_freq", torch.float32, half), _is(slots, "slots", torch.int64, n),
+               _is(positions, "positions", torch.int32, n),
+               _is(tokens, "tokens", torch.int64, n), rec[0], rec[1],
+               _is(q_out, "q_out", dt, n, hq, d), float(eps), 2 * half, int(bool(interleaved)))
+    return load().arbor_append(ctypes.byref(g), ctypes.byref(t), ctypes.byref(p), int(layer),
+                               ctypes.byref(a), n, _is(status, "status", torch.int32, 1),
+                               _stream(stream))
+
+
+def arbor_prefill_plan_size(kv: KVState, n_seq: int, n_tokens: int) -> int:
+    g = kv.geom()
+    return int(load().arbor_prefill_plan_size(ctypes.byref(g), int(n_seq), int(n_tokens)))
+
+
+def arbor_prefill_workspace_size(kv: KVState, n_seq: int, n_tokens: int) -> int:
+    g = kv.geom()
+    return int(load().arbor_prefill_workspace_size(ctypes.byref(g), int(n_seq), int(n_tokens)))
+
+
+def arbor_prefill_plan(kv: KVState, nodes, cu, n_tokens, plan, status, stream=None) -> int:
+    """The work list of arbor_tree_prefill_attn for the newest tokens of blocks, into
+    `plan` (arbor_prefill_plan_size bytes)."""
+    g, t = kv.geom(), kv.tree()
+    n_seq, nd, c = _packed(nodes, cu)
+    return load().arbor_prefill_plan(ctypes.byref(g), ctypes.byref(t), nd, n_seq, c, int(n_tokens),
+                                     _dev(plan, "plan"), int(plan.numel()),
+                                     _is(status, "status", torch.int32, 1), _stream(stream))
+
+
+def arbor_tree_prefill_attn(kv: KVState, plan, n_seq, layer, q, out, lse_out, softmax_scale,
+                            status, workspace, stream=None, timing=None) -> int:
+    """Causal attention of the packed tokens q [n_tokens, Hq, head_dim] over their
+    chains, by the plan made for them."""
+    g, t, p = kv.geom(timing), kv.tree(), kv.pool()
+    n, hq, dt = int(q.shape[0]), kv.kv_heads * kv.q_per_kv, _element(kv)
+    return load().arbor_tree_prefill_attn(ctypes.byref(g), ctypes.byref(t), ctypes.byref(p),
+                                          _dev(plan, "plan"), int(plan.numel()), int(n_seq), n,
+                                          int(layer), _is(q, "q", dt, n, hq, kv.head_dim),
+                                          _is(out, "out", dt, n, hq, kv.head_dim),
+                                          _is(lse_out, "lse_out", torch.float32, n, hq),
+                                          float(softmax_scale),
+                                          _is(status, "status", torch.int32, 1),
+                                          _dev(workspace, "workspace"), int(workspace.numel()),
+                                          _stream(stream))

@@ -29,6 +29,25 @@ int launch_decode(const arbor_geom_t *, const arbor_tree_t *, const arbor_pool_t
 int launch_uncertainty(const void *, int32_t, int32_t, int64_t, int32_t, const int32_t *, float *,
                        int32_t, int32_t *, void *, size_t, hipStream_t);
 size_t uncertainty_workspace(int32_t, int64_t, int32_t);
+int launch_extend(const arbor_geom_t *, arbor_tree_t *, arbor_pool_t *, int32_t *, const int32_t *,
+                  int32_t, const int32_t *, int32_t, int64_t *, int32_t *, int64_t *, int32_t *,
+                  void *, size_t, hipStream_t);
+int launch_truncate(const arbor_geom_t *, arbor_tree_t *, arbor_pool_t *, int32_t *,
+                    const int32_t *, const int32_t *, int32_t, int32_t *, void *, size_t,
+                    hipStream_t);
+int launch_fork(const arbor_geom_t *, arbor_tree_t *, arbor_pool_t *, int32_t *, const int32_t *,
+                const int32_t *, int32_t, float *, int64_t *, int32_t *, void *, size_t,
+                hipStream_t);
+int launch_append(const arbor_geom_t *, const arbor_tree_t *, arbor_pool_t *, int32_t,
+                  const arbor_append_t *, int32_t, int32_t *, hipStream_t);
+size_t prefill_plan_size(const arbor_geom_t *, int32_t, int32_t);
+size_t prefill_workspace_size(const arbor_geom_t *, int32_t, int32_t);
+int launch_prefill_plan(const arbor_geom_t *, const arbor_tree_t *, const int32_t *, int32_t,
+                        const int32_t *, int32_t, void *, size_t, int32_t *, hipStream_t);
+int launch_prefill(const arbor_geom_t *, const arbor_tree_t *, const arbor_pool_t *, const void *,
+                   size_t, int32_t, int32_t, int32_t, const void *, void *, float *, float,
+                   int32_t *, void *, size_t, hipStream_t);
+size_t pages_workspace(const arbor_sizes_t *);
 size_t score_workspace(const arbor_geom_t *, const arbor_sizes_t *);
 size_t allocate_workspace(const arbor_sizes_t *);
 size_t compact_workspace(const arbor_sizes_t *);
@@ -95,10 +114,10 @@ extern "C" {
 size_t arbor_workspace_size(const arbor_geom_t *geom, const arbor_sizes_t *sz) {
   if (!geom || !sz) return 0;
   size_t b = 0;
-  const size_t parts[5] = {score_workspace(geom, sz), allocate_workspace(sz),
+  const size_t parts[6] = {score_workspace(geom, sz), allocate_workspace(sz),
                            compact_workspace(sz), rehydrate_workspace(sz),
-                           decode_workspace(geom, sz)};
-  for (size_t e = 0; e < 5; ++e) b = parts[e] > b ? parts[e] : b;
+                           decode_workspace(geom, sz), pages_workspace(sz)};
+  for (size_t e = 0; e < 6; ++e) b = parts[e] > b ? parts[e] : b;
   return b + 65536;
 }
 
@@ -269,6 +288,123 @@ int arbor_uncertainty(const void *logits, int32_t dtype, int32_t n_rows, int64_t
     return ARBOR_EUNSUPPORTED;
   return launch_uncertainty(logits, dtype, n_rows, vocab, top_k, dst, u_out, n_out, status,
                             workspace, workspace_bytes, stream);
+}
+
+// What arbor_extend, arbor_truncate and arbor_fork have in common: n_full names the
+// array that the tree reads, and a list of ascending ids is no longer than the tree.
+static int check_grow(const arbor_geom_t *geom, const arbor_tree_t *tree, const arbor_pool_t *pool,
+                      const int32_t *n_full, int32_t n_list, const int32_t *status) {
+  ARBOR_TRY(check_geom(geom));
+  ARBOR_TRY(check_tree(tree));
+  ARBOR_TRY(check_pool(pool));
+  if (!status || n_full != tree->n_full || n_list < 0 || n_list > tree->num_nodes)
+    return ARBOR_EINVAL;
+  return ARBOR_OK;
+}
+
+int arbor_extend(const arbor_geom_t *geom, arbor_tree_t *tree, arbor_pool_t *pool,
+                 int32_t *n_full, const int32_t *nodes, int32_t n_seq, const int32_t *cu,
+                 int32_t n_tokens, int64_t *slots, int32_t *positions, int64_t *tokens,
+                 int32_t *status, void *workspace, size_t workspace_bytes, hipStream_t stream) {
+  ARBOR_TRY(check_grow(geom, tree, pool, n_full, n_seq, status));
+  if (n_tokens < 0) return ARBOR_EINVAL;
+  if (n_tokens == 0) return ARBOR_OK;
+  if (!cu || !slots || !positions || (n_seq > 0 && !nodes)) return ARBOR_EINVAL;
+  return launch_extend(geom, tree, pool, n_full, nodes, n_seq, cu, n_tokens, slots, positions,
+                       tokens, status, workspace, workspace_bytes, stream);
+}
+
+int arbor_truncate(const arbor_geom_t *geom, arbor_tree_t *tree, arbor_pool_t *pool,
+                   int32_t *n_full, const int32_t *nodes, const int32_t *keep, int32_t n_nodes,
+                   int32_t *status, void *workspace, size_t workspace_bytes, hipStream_t stream) {
+  ARBOR_TRY(check_grow(geom, tree, pool, n_full, n_nodes, status));
+  if (n_nodes > 0 && (!nodes || !keep)) return ARBOR_EINVAL;
+  return launch_truncate(geom, tree, pool, n_full, nodes, keep, n_nodes, status, workspace,
+                         workspace_bytes, stream);
+}
+
+int arbor_fork(const arbor_geom_t *geom, arbor_tree_t *tree, arbor_pool_t *pool,
+               int32_t *n_full, const int32_t *src, const int32_t *dst, int32_t n_forks, float *A,
+               int64_t *rows_seen, int32_t *status, void *workspace, size_t workspace_bytes,
+               hipStream_t stream) {
+  ARBOR_TRY(check_grow(geom, tree, pool, n_full, n_forks, status));
+  if (n_forks > 0 && (!src || !dst)) return ARBOR_EINVAL;
+  return launch_fork(geom, tree, pool, n_full, src, dst, n_forks, A, rows_seen, status, workspace,
+                     workspace_bytes, stream);
+}
+
+int arbor_append(const arbor_geom_t *geom, const arbor_tree_t *tree, arbor_pool_t *pool,
+                 int32_t layer, const arbor_append_t *a, int32_t n_tokens, int32_t *status,
+                 hipStream_t stream) {
+  ARBOR_TRY(check_geom(geom));
+  if (!tree || tree->num_tokens < 0 || !pool || !pool->k || !pool->v || !a || !status)
+    return ARBOR_EINVAL;
+  if (n_tokens < 0 || layer < 0 || layer >= geom->num_layers) return ARBOR_EINVAL;
+  if (n_tokens == 0) return ARBOR_OK;
+  if (!a->q || !a->k || !a->v || !a->q_out || !a->slots || !a->positions) return ARBOR_EINVAL;
+  const int64_t d = geom->head_dim, kv = geom->num_kv_heads * d, qw = kv * geom->q_per_kv;
+  if (a->q_stride < qw || a->k_stride < kv || a->v_stride < kv) return ARBOR_EINVAL;
+  if (a->interleaved != 0 && a->interleaved != 1) return ARBOR_EINVAL;
+  if (a->rotary_dim < 0 || (a->rotary_dim > 0 && !a->inv_freq) || !(a->eps >= 0.0f))
+    return ARBOR_EINVAL;
+  if ((a->record_k != nullptr) != (a->record_v != nullptr) || (a->record_k && !a->tokens))
+    return ARBOR_EINVAL;
+  if (a->q_out == a->q && a->q_stride != qw) return ARBOR_EINVAL;
+  if (a->rotary_dim % 8 != 0 || a->rotary_dim > geom->head_dim) return ARBOR_EUNSUPPORTED;
+  const int64_t per16 = geom->dtype == ARBOR_BF16 ? 8 : 4;
+  const void *ptrs[] = {a->q, a->k, a->v, a->q_out, a->q_norm, a->k_norm, a->record_k, a->record_v,
+                        pool->k, pool->v};
+  for (const void *p : ptrs)
+    if (reinterpret_cast<uintptr_t>(p) % 16 != 0) return ARBOR_EUNSUPPORTED;
+  if (a->q_stride % per16 || a->k_stride % per16 || a->v_stride % per16) return ARBOR_EUNSUPPORTED;
+  return launch_append(geom, tree, pool, layer, a, n_tokens, status, stream);
+}
+
+// Shapes of the prefill calls: more than 128 query heads for a KV head do not fit a tile.
+static int check_prefill(const arbor_geom_t *geom, int32_t n_seq, int32_t n_tokens) {
+  ARBOR_TRY(check_geom(geom));
+  if (n_seq < 0 || n_tokens < 0) return ARBOR_EINVAL;
+  if (geom->q_per_kv > 128) return ARBOR_EUNSUPPORTED;
+  return ARBOR_OK;
+}
+
+size_t arbor_prefill_plan_size(const arbor_geom_t *geom, int32_t n_seq, int32_t n_tokens) {
+  if (check_prefill(geom, n_seq, n_tokens) != ARBOR_OK) return 0;
+  return prefill_plan_size(geom, n_seq, n_tokens);
+}
+
+size_t arbor_prefill_workspace_size(const arbor_geom_t *geom, int32_t n_seq, int32_t n_tokens) {
+  if (check_prefill(geom, n_seq, n_tokens) != ARBOR_OK) return 0;
+  return prefill_workspace_size(geom, n_seq, n_tokens);
+}
+
+int arbor_prefill_plan(const arbor_geom_t *geom, const arbor_tree_t *tree, const int32_t *nodes,
+                       int32_t n_seq, const int32_t *cu, int32_t n_tokens, void *plan,
+                       size_t plan_bytes, int32_t *status, hipStream_t stream) {
+  ARBOR_TRY(check_prefill(geom, n_seq, n_tokens));
+  ARBOR_TRY(check_tree(tree));
+  if (!status || !plan || reinterpret_cast<uintptr_t>(plan) % 256 != 0) return ARBOR_EINVAL;
+  if (n_tokens > 0 && n_seq > 0 && (!nodes || !cu)) return ARBOR_EINVAL;
+  return launch_prefill_plan(geom, tree, nodes, n_seq, cu, n_tokens, plan, plan_bytes, status,
+                             stream);
+}
+
+int arbor_tree_prefill_attn(const arbor_geom_t *geom, const arbor_tree_t *tree,
+                            const arbor_pool_t *pool, const void *plan, size_t plan_bytes,
+                            int32_t n_seq, int32_t n_tokens, int32_t layer, const void *q,
+                            void *out, float *lse_out, float softmax_scale, int32_t *status,
+                            void *workspace, size_t workspace_bytes, hipStream_t stream) {
+  ARBOR_TRY(check_prefill(geom, n_seq, n_tokens));
+  ARBOR_TRY(check_tree(tree));
+  ARBOR_TRY(check_pool(pool));
+  if (!status || !plan || reinterpret_cast<uintptr_t>(plan) % 256 != 0) return ARBOR_EINVAL;
+  if (layer < 0 || layer >= geom->num_layers) return ARBOR_EINVAL;
+  if (n_tokens > 0 && n_seq > 0 && (!q || !out || !workspace)) return ARBOR_EINVAL;
+  const void *ptrs[] = {q, out, pool->k, pool->v, workspace};
+  for (const void *p : ptrs)
+    if (reinterpret_cast<uintptr_t>(p) % 16 != 0) return ARBOR_EUNSUPPORTED;
+  return launch_prefill(geom, tree, pool, plan, plan_bytes, n_seq, n_tokens, layer, q, out, lse_out,
+                        softmax_scale, status, workspace, workspace_bytes, stream);
 }
 
 }  // extern "C"

@@ -1,0 +1,929 @@
+// arbor_prefill_plan and arbor_tree_prefill_attn: causal attention of the packed new
+// tokens of several blocks over their root-to-leaf chains (Sec. 1, Sec. 3).
+//
+// A tile is up to kRows query rows of one KV head: consecutive packed tokens, of
+// one block or of several, times their G query heads.  Its keys are the union of
+// its blocks' chains, in 16-slot sub-pages; each chain block carries the set of
+// the tile's sequences below it, so that tokens of several blocks share the reads
+// of the ancestors they have in common, and a row sees a key when its sequence is
+// in the block's set and, in its own block, the slot is not after its own.
+//
+// The plan (three launches, once for all layers): cut the packed tokens into tiles;
+// a wave per tile merges its chains; split the tiles whose keys outlast the others'
+// into parts, so that a few rows over a long prompt fill the chip.  The attention
+// runs one workgroup per (part, KV head) and a second launch joins the parts.
+//
+// Attention of a tile: a wave holds 32 rows.  S^T = K Q^T with 32x32 MFMA leaves
+// each lane one row and half of the keys, so the softmax needs one exchange between
+// two lanes only where a row's reference max moves; O^T += V^T P^T takes P as the B
+// operand straight from those registers (the order of the keys within a step is the
+// one in which S^T leaves them; V^T is read from LDS in the same order, through the
+// transposing LDS read for bf16).  Keys and values come by direct loads to LDS
+// through a buffer resource over the valid rows of a sub-page, which fills the
+// others with zeros.
+#include <type_traits>
+
+#include "arbor_internal.h"
+#include "mfma_ops.h"
+
+namespace arbor {
+
+namespace {
+
+constexpr int kRows = 128;              // query rows of a tile: four waves of 32
+constexpr int kWaves = kRows / 32;
+constexpr int kMaxSeq = 64;             // sequences of a tile: one bit each
+constexpr int MAXD = ARBOR_MAX_DEPTH + 1;
+constexpr int kEntLds = 128;            // chain blocks of a tile that are kept in LDS
+constexpr int64_t kMagic = 0x61726270726c6601;
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kLn2 = 0.6931471805599453f;
+// A row's reference max moves when the terms of some lane add up to more than this:
+// until then p = 2^(s - ref) may exceed 1, which costs no precision in fp32 or bf16
+// and leaves V 2^100 of headroom, and a step needs neither a max nor a rescale.
+constexpr float kMoveAt = 65536.0f;
+// Workgroups that the chip holds at a time (two to each of 256 CUs)
+constexpr int kSlots = 512;
+constexpr int kMinPart = 32;            // sub-pages of the shortest part
+
+struct Header {
+  int64_t magic;
+  int32_t n_seq, n_tokens, V, G, Hkv, page_size, n_tiles, n_units, n_split;
+};
+
+struct Tile {
+  int32_t t0, nt;       // packed tokens
+  int32_t e0, ne;       // sequences that they belong to
+  int32_t n_ent;        // chain blocks, at entry kMaxSeq... (see entry_base)
+  int32_t n_sub;        // sub-pages of all of them
+  int32_t parts;        // 1: written directly
+  int32_t part0;        // first partial
+};
+
+// One chain block of a tile, root first.
+struct __attribute__((aligned(16))) Entry {
+  int32_t node;
+  int32_t limit;        // slots that some row of the tile sees
+  int32_t sub0;         // sub-pages of the blocks before it
+  int32_t po;           // its first page-table entry
+  uint64_t below;       // the tile's sequences whose chain holds it
+  uint64_t own;         // those whose own block it is
+};
+
+struct Unit {
+  int32_t tile, s0, s1, part;   // sub-pages [s0, s1); part -1: the whole tile
+};
+
+struct PlanPtrs {
+  Header *head;
+  Tile *tiles;
+  Entry *ents;
+  Unit *units;
+  int32_t *split;       // tiles in parts
+  int2 *tok;            // per packed token: own slot, sequence within its tile
+  int64_t tiles_cap, units_cap;
+};
+
+__host__ __device__ inline int tokens_per_tile(int G) { return kRows / G; }
+
+// Bounds on the tiles and units of a call, known to the host.
+inline int64_t tile_bound(int G, int n_seq, int64_t n_tokens) {
+  // two neighbouring tiles hold more tokens than one may, or end a run of 64 sequences
+  const int64_t b = 2 * (n_tokens / tokens_per_tile(G)) + n_seq / kMaxSeq + 2;
+  return b < n_tokens ? b : n_tokens;
+}
+inline int target_parts(int Hkv) {
+  const int t = kSlots / Hkv;
+  return t > 0 ? t : 1;
+}
+
+PlanPtrs carve_plan(const arbor_geom_t *g, int n_seq, int n_tokens, void *plan, size_t bytes,
+                    size_t *need) {
+  PlanPtrs p{};
+  p.tiles_cap = tile_bound(g->q_per_kv, n_seq, n_tokens);
+  p.units_cap = p.tiles_cap + target_parts(g->num_kv_heads) + 1;
+  Carve cv(plan, bytes);
+  p.head = cv.take<Header>(1);
+  p.tiles = cv.take<Tile>(p.tiles_cap + 1);
+  p.ents = cv.take<Entry>((size_t)kMaxSeq * ((size_t)n_seq + p.tiles_cap + 1));
+  p.units = cv.take<Unit>(p.units_cap);
+  p.split = cv.take<int32_t>(target_parts(g->num_kv_heads) + 1);
+  p.tok = cv.take<int2>((size_t)n_tokens + 1);
+  if (need) *need = cv.off;
+  if (!cv.ok) p.head = nullptr;
+  return p;
+}
+
+// A tile's region of the entries: a chain has at most MAXD = kMaxSeq blocks, and the
+// (tile, sequence) pairs before tile k are at most e0 + k.
+static_assert(MAXD == kMaxSeq, "entry regions");
+__host__ __device__ inline int64_t entry_base(int tile, int e0) {
+  return (int64_t)kMaxSeq * (e0 + tile);
+}
+
+// ---- plan ---------------------------------------------------------------------
+// Cuts the packed tokens into tiles.  A tile takes the next block's tokens when all
+// of them fit (two blocks in one tile read the blocks that they share once, and
+// nothing twice); a block of more tokens than a tile holds starts its own.  One
+// wave goes from tile to tile, 64 blocks at a time in its lanes.
+__global__ __launch_bounds__(1024) void plan_tiles(Tree t, int G, int Hkv, int P,
+                                                   const int32_t *__restrict__ nodes, int n_seq,
+                                                   const int32_t *__restrict__ cu, int n_tokens,
+                                                   PlanPtrs p, int32_t *status) {
+  if (threadIdx.x == 0) p.head->magic = 0;
+  if (status_failed(status)) return;
+  int err = 0;
+  if (threadIdx.x == 0 && (cu[0] != 0 || cu[n_seq] < 0 || cu[n_seq] > n_tokens)) err = 1;
+  for (int e = threadIdx.x; e < n_seq; e += blockDim.x) {
+    const int i = nodes[e], m = cu[e + 1] - cu[e];
+    if (i < 0 || i >= t.V || m < 0 || m > n_tokens) err = 1;
+    else if (m > t.n_kept[i]) err = 1;
+  }
+  if (__syncthreads_or(err)) {
+    if (threadIdx.x == 0) status_error(status, ARBOR_EINVAL);
+    return;
+  }
+  if (threadIdx.x >= kWave) return;
+  const int lane = lane_id(), TQ = tokens_per_tile(G);
+  int e = 0, off = 0, k = 0;               // off: tokens of sequence e already in tiles
+  while (e < n_seq) {
+    const int c0 = e + lane < n_seq ? cu[e + lane] : 0;
+    const int c1 = e + lane < n_seq ? cu[e + lane + 1] : 0;
+    const int m = e + lane < n_seq ? c1 - c0 - (lane == 0 ? off : 0) : TQ + 1;
+    const int first = lane_value(m, 0), t0 = lane_value(c0, 0) + off;
+    if (first == 0) {
+      const uint64_t some = ballot(m != 0);
+      e += some ? __builtin_ctzll(some) : kWave;
+      off = 0;
+      continue;
+    }
+    if (first > TQ) {
+      const int full = first / TQ;
+      for (int x = lane; x < full; x += kWave)
+        if (k + x < p.tiles_cap) p.tiles[k + x] = Tile{t0 + x * TQ, TQ, e, 1, 0, 0, 1, 0};
+      k += full;
+      off += full * TQ;
+      if (full * TQ == first) {
+        ++e;
+        off = 0;
+      }
+      continue;
+    }
+    const int sum = wave_inclusive_scan(min(m, TQ + 1));
+    const int fit = popc(ballot(sum <= TQ));          // sums ascend
+    const int nt = lane_value(sum, fit - 1);
+    if (lane == 0 && k < p.tiles_cap) p.tiles[k] = Tile{t0, nt, e, fit, 0, 0, 1, 0};
+    ++k;
+    e += fit;
+    off = 0;
+  }
+  if (lane == 0) {
+    if (k > p.tiles_cap) status_error(status, ARBOR_ECORRUPT);   // (the bound holds)
+    p.head->n_seq = n_seq;
+    p.head->n_tokens = n_tokens;
+    p.head->V = t.V;
+    p.head->G = G;
+    p.head->Hkv = Hkv;
+    p.head->page_size = P;
+    p.head->n_tiles = k;
+  }
+}
+
+// One wave per tile: the chains of its sequences, merged by ascending id.
+__global__ __launch_bounds__(64) void plan_chains(Tree t, const int32_t *__restrict__ nodes,
+                                                  const int32_t *__restrict__ cu, PlanPtrs p,
+                                                  int32_t *status) {
+  __shared__ int32_t chain[MAXD][kWave + 1];     // leaf first
+  if (status_failed(status) || (int)blockIdx.x >= p.head->n_tiles) return;
+  const int lane = lane_id();
+  Tile tl = p.tiles[blockIdx.x];
+  Entry *ents = p.ents + entry_base(blockIdx.x, tl.e0);
+  const int e = tl.e0 + lane;
+  int lo = 0, hi = 0, x = -1, newest = -1;
+  if (lane < tl.ne) {
+    const int c0 = cu[e], c1 = cu[e + 1];
+    lo = max(c0, tl.t0);
+    hi = min(c1, tl.t0 + tl.nt);
+    if (hi > lo) {
+      x = nodes[e];
+      newest = t.n_kept[x] - (c1 - hi) - 1;       // slot of the sequence's last token here
+    }
+  }
+  const int leaf = x;
+  int depth = 0;
+  bool bad = false, deep = false;
+  for (int y = x; ballot(y >= 0);) {
+    if (y >= 0) {
+      chain[depth][lane] = y;
+      ++depth;
+      const int up = t.parent[y];
+      if (up >= y) bad = true;
+      else if (up >= 0 && depth == MAXD) deep = true;
+      y = bad || deep ? -1 : up;
+    }
+  }
+  if (ballot(bad || deep)) {
+    if (lane == 0) status_error(status, ballot(bad) ? ARBOR_EINVAL : ARBOR_EUNSUPPORTED);
+    return;
+  }
+  // the smallest id among the lanes' next blocks, until none is left
+  int at = depth - 1, n = 0;
+  while (true) {
+    const int next = at >= 0 ? chain[at][lane] : INT32_MAX;
+    const int mn = wave_allreduce(next, [](int a, int b) { return a < b ? a : b; });
+    if (mn == INT32_MAX) break;
+    const bool here = next == mn;
+    const uint64_t below = ballot(here), own = ballot(here && mn == leaf);
+    const int last = wave_allreduce(here && mn == leaf ? newest : -1,
+                                    [](int a, int b) { return a > b ? a : b; });
+    if (lane == 0) {
+      ents[n].node = mn;
+      ents[n].limit = last + 1;
+      ents[n].below = below;
+      ents[n].own = own;
+    }
+    at -= here ? 1 : 0;
+    ++n;
+  }
+  __threadfence_block();
+  __builtin_amdgcn_wave_barrier();
+  int subs = 0;
+  for (int b = 0; b < n; b += kWave) {
+    const int y = b + lane;
+    int mine = 0;
+    if (y < n) {
+      const int node = ents[y].node;
+      const int limit = ents[y].below == ents[y].own ? ents[y].limit : t.n_kept[node];
+      ents[y].limit = limit;
+      ents[y].po = (int32_t)t.page_off[node];
+      mine = (limit + 15) / 16;
+    }
+    const int inc = wave_inclusive_scan(mine);
+    if (y < n) ents[y].sub0 = subs + inc - mine;
+    subs += lane_value(inc, kWave - 1);
+  }
+  if (lane == 0) {
+    p.tiles[blockIdx.x].n_ent = n;
+    p.tiles[blockIdx.x].n_sub = subs;
+  }
+  // own slot and sequence of each of its tokens
+  for (int j = 0; j < tl.ne; ++j) {
+    const int l = lane_value(lo, j), h = lane_value(hi, j), last = lane_value(newest, j);
+    for (int y = l + lane; y < h; y += kWave) p.tok[y] = int2{last - (h - 1 - y), j};
+  }
+}
+
+// Parts of the tiles, longest first.
+__global__ __launch_bounds__(1024) void plan_units(PlanPtrs p, int target, int32_t *status) {
+  constexpr int NB = 256;
+  __shared__ int64_t sm[17];
+  __shared__ int32_t bucket[NB + 1];
+  if (status_failed(status)) return;
+  const int n = p.head->n_tiles, nt = blockDim.x, tid = threadIdx.x;
+  const int per = (n + nt - 1) / nt;
+  const int r0 = min(n, tid * per), r1 = min(n, r0 + per);
+  int64_t subs = 0;
+  for (int k = r0; k < r1; ++k) subs += p.tiles[k].n_sub;
+  const int64_t total = block_sum(subs, sm);
+  const int64_t even = (total + target - 1) / target;
+  const int most = (int)(even > kMinPart ? even : kMinPart);
+  for (int b = tid; b <= NB; b += nt) bucket[b] = 0;
+  __syncthreads();
+  int64_t parts = 0, cut = 0;
+  for (int k = r0; k < r1; ++k) {
+    const int s = p.tiles[k].n_sub, np = s > most ? (s + most - 1) / most : 1;
+    p.tiles[k].parts = np;
+    if (np > 1) {
+      parts += np;
+      ++cut;
+    }
+    // (a part has at most `most` sub-pages, a tile in parts too)
+    atomicAdd(&bucket[NB - 1 - (int)((int64_t)((s + np - 1) / np) * (NB - 1) / most)], np);
+  }
+  int64_t n_parts, n_cut;
+  int64_t part0 = block_exclusive_scan(parts, sm, &n_parts);
+  int64_t cut0 = block_exclusive_scan(cut, sm, &n_cut);
+  __syncthreads();
+  if (tid < kWave) {
+    int base = 0;
+    for (int b = 0; b < NB; b += kWave) {
+      const int v = bucket[b + tid];
+      const int inc = wave_inclusive_scan(v);
+      bucket[b + tid] = base + inc - v;
+      base += lane_value(inc, kWave - 1);
+    }
+    if (tid == 0) bucket[NB] = base;
+  }
+  __syncthreads();
+  const int units = bucket[NB];
+  __syncthreads();
+  for (int k = r0; k < r1; ++k) {
+    const int s = p.tiles[k].n_sub, np = p.tiles[k].parts;
+    const int len = (s + np - 1) / np;
+    const int b = NB - 1 - (int)((int64_t)len * (NB - 1) / most);
+    if (np > 1) {
+      p.tiles[k].part0 = (int32_t)part0;
+      if (cut0 < target) p.split[cut0] = k;
+      ++cut0;
+    }
+    const int u0 = atomicAdd(&bucket[b], np);
+    for (int x = 0; x < np; ++x) {
+      // even parts of whole steps where they are long
+      const int a = (int)((int64_t)s * x / np), z = (int)((int64_t)s * (x + 1) / np);
+      if (u0 + x < p.units_cap)
+        p.units[u0 + x] = Unit{k, a, z, np > 1 ? (int32_t)part0 + x : -1};
+    }
+    if (np > 1) part0 += np;
+  }
+  if (tid == 0) {
+    p.head->n_units = units;
+    p.head->n_split = (int)n_cut;
+    if (units > p.units_cap || n_cut > target) status_error(status, ARBOR_ECORRUPT);
+    else p.head->magic = kMagic;
+  }
+}
+
+// ---- attention -------------------------------------------------------------------
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) void *LdsPtr;
+
+// What the two element types differ in.  KS: MFMA steps over head_dim; a lane's
+// operand of step ks are the elements 16-byte piece 2 (ks / SPP) + h of a row, h the
+// lane's half of the wave.
+template <class T, int D>
+struct Cfg {
+  static constexpr int ES = (int)sizeof(T);
+  static constexpr int ROW = D * ES;                     // bytes of a row
+  static constexpr int PIECES = ROW / 16;
+  static constexpr int SUBS = ES == 2 ? 4 : 2;           // sub-pages of a step
+  static constexpr int KEYS = 16 * SUBS;
+  static constexpr int NS = KEYS / 32;                   // 32-key tiles of S
+  static constexpr int BUF = KEYS * ROW;                 // K (or V) of a step
+  static constexpr int LPW = SUBS * 2 * 16 * ROW / 1024 / kWaves;   // 1 KB loads of a wave
+  static constexpr int LPS = 16 * ROW / 1024;            // of a sub-page
+  static constexpr int DT = D / 32;
+  static constexpr int NQ = ROW / 32;                    // 16-byte operand pieces of a lane
+  static constexpr int LDS = 4 * BUF;
+};
+
+// Where piece x of row r of a step's K lies: rows 0..15 (of 16-lane groups that read
+// one piece) fall on distinct banks.
+template <class T, int D>
+__device__ __forceinline__ int k_piece(int r, int x) {
+  constexpr int N = Cfg<T, D>::PIECES;
+  if constexpr (N == 8) return x ^ ((r >> 1) & 7);
+  else return x ^ (r & (N - 1) & 31);
+}
+// The same of V: the four rows that a transposing read takes 64 bytes of (bf16), or
+// the two rows of an fp32 read, fall on distinct banks.
+template <class T, int D>
+__device__ __forceinline__ int v_piece(int r, int x) {
+  constexpr int N = Cfg<T, D>::PIECES;
+  if constexpr (sizeof(T) == 4) return x ^ (((r >> 2) & 1) << 3);
+  else if constexpr (N == 8) return x ^ (((r >> 1) & 1) << 2);
+  else return x ^ ((r & 3) << 2);
+}
+
+struct AttnArgs {
+  Tree t;
+  Pool pl;
+  PlanPtrs p;
+  int n_seq, n_tokens, layer;
+  const void *q;
+  void *out;
+  float *lse;
+  float sl2;            // softmax scale in log2 units
+  float *part;          // [parts][Hkv][kRows][D + 2]
+  int64_t part_cap;     // parts that it holds
+  int32_t *status;
+};
+
+// Direct loads to LDS of the rows of one sub-page, `bytes` of which are valid: 16
+// bytes a lane, load c to dst + 1024 c.  The buffer resource (scalar registers)
+// bounds every access; beyond it zeros are written.
+// (host-device so the kernel's host-device lambdas can call it; the host pass of the
+// compiler never runs it)
+template <int N>
+__host__ __device__ __forceinline__ void load_sub_page(const char *src, int bytes, char *dst,
+                                                       const int (&off)[N]) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  const __amdgpu_buffer_rsrc_t rsrc =
+      __builtin_amdgcn_make_buffer_rsrc(const_cast<char *>(src), 0, bytes, 0x00020000);
+#pragma unroll
+  for (int c = 0; c < N; ++c)
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (LdsPtr)(dst + 1024 * c), 16, off[c], 0, 0, 0);
+#endif
+}
+
+__device__ __forceinline__ float swap_halves_add(float v) {
+  float a, b;
+  row_swap<true>(v, a, b);
+  return a + b;
+}
+__device__ __forceinline__ float swap_halves_max(float v) {
+  float a, b;
+  row_swap<true>(v, a, b);
+  return fmaxf(a, b);
+}
+
+// One sub-page per lane, 64 of them: read by readlane.
+struct Window {
+  int page, info, slot, ent;     // info: first row | valid rows << 8 | flags << 16
+};
+constexpr int kMask = 1 << 16;   // some row of this wave must not see some key of it
+constexpr int kNone = 1 << 17;   // no row of this wave sees any
+
+__device__ __forceinline__ bool header_ok(const AttnArgs &a) {
+  const Header *h = a.p.head;
+  return h->magic == kMagic && h->n_seq == a.n_seq && h->n_tokens == a.n_tokens &&
+         h->V == a.t.V && h->G == a.pl.G && h->Hkv == a.pl.Hkv && h->page_size == a.pl.P;
+}
+
+template <class T, int D>
+__global__ __launch_bounds__(kRows * 2, 2) void prefill_attn(AttnArgs a) {
+  typedef Cfg<T, D> C;
+  extern __shared__ __attribute__((aligned(16))) char lds[];
+  __shared__ Entry sh_ent[kEntLds];
+  const Pool &pl = a.pl;
+  if (status_failed(a.status)) return;
+  if (!header_ok(a)) {
+    if (blockIdx.x == 0 && threadIdx.x == 0) status_error(a.status, ARBOR_EINVAL);
+    return;
+  }
+  const int g = blockIdx.x % pl.Hkv, u = blockIdx.x / pl.Hkv;
+  if (u >= a.p.head->n_units) return;
+  const Unit un = a.p.units[u];
+  const Tile tl = a.p.tiles[un.tile];
+  const Entry *ents = a.p.ents + entry_base(un.tile, tl.e0);
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int lr = lane & 31, h = lane >> 5;
+  const bool ents_lds = tl.n_ent <= kEntLds;
+  for (int x = tid; x < tl.n_ent && ents_lds; x += kRows * 2) sh_ent[x] = ents[x];
+  __syncthreads();
+
+  // this lane's row
+  const int G = pl.G, row = wave * 32 + lr;
+  const int tq = row / G;
+  const bool live = tq < tl.nt;
+  const int tok = tl.t0 + (live ? tq : 0);
+  const int head = g * G + (live ? row - tq * G : 0);
+  const int2 info = a.p.tok[tok];
+  const int qslot = info.x;
+  const uint64_t seq_bit = live ? 1ull << (info.y & 63) : 0;
+  const bool any_live = wave * 32 / G < tl.nt;
+  // sequences and own slots of the wave's rows
+  uint64_t seqs = wave_allreduce(seq_bit, [](uint64_t x, uint64_t y) { return x | y; });
+  const int qmin = wave_allreduce(live ? qslot : INT32_MAX,
+                                  [](int x, int y) { return x < y ? x : y; });
+  const int qmax = wave_allreduce(live ? qslot : -1, [](int x, int y) { return x > y ? x : y; });
+
+  const int Hq = pl.Hkv * G;
+  // Q as the B operand: its row, pieces 2 i + h
+  typedef typename std::conditional<sizeof(T) == 2, bf16x8, f32x4>::type qvec;
+  qvec qf[C::NQ];
+  {
+    const T *qp = static_cast<const T *>(a.q) + ((int64_t)tok * Hq + head) * D;
+#pragma unroll
+    for (int i = 0; i < C::NQ; ++i)
+      qf[i] = *reinterpret_cast<const qvec *>(qp + (2 * i + h) * (16 / C::ES));
+  }
+
+  const int n_sub = un.s1 - un.s0;
+  const int steps = (n_sub + C::SUBS - 1) / C::SUBS;
+  constexpr int WSTEPS = kWave / C::SUBS;         // steps of a window
+  // sub-page w0 + lane of the unit
+  bool stale = false;
+  auto fill = [&](int w0) -> Window {
+    const int sp = un.s0 + w0 + lane;
+    Window w{0, kNone, 0, 0};
+    if (sp >= un.s1) return w;
+    int lo = 0, hi = tl.n_ent;
+    while (hi - lo > 1) {
+      const int mid = (lo + hi) / 2;
+      const int first = ents_lds ? sh_ent[mid].sub0 : ents[mid].sub0;
+      if (first <= sp) lo = mid;
+      else hi = mid;
+    }
+    // (a block without a slot to see starts where the next one does: the last wins)
+    const Entry en = ents_lds ? sh_ent[lo] : ents[lo];
+    w.ent = lo;
+    w.slot = (sp - en.sub0) * 16;
+    int page = a.t.page_table[(int64_t)en.po + w.slot / pl.P];
+    const int valid = min(16, en.limit - w.slot);
+    if (page < 0 || page >= pl.num_pages) {       // the tree has changed since the plan
+      stale = true;
+      page = 0;
+    }
+    w.page = page;
+    int flags = 0;
+    const uint64_t mine = en.below & seqs, mown = en.own & seqs;
+    if (mine == 0 || (mine == mown && w.slot > qmax)) flags = kNone;
+    else if (mine != seqs || valid < 16 || (mown && w.slot + 15 > qmin)) flags = kMask;
+    w.info = w.slot % pl.P | valid << 8 | flags;
+    return w;
+  };
+
+  const char *kpool = static_cast<const char *>(pl.k);
+  const char *vpool = static_cast<const char *>(pl.v);
+  // this wave's direct loads of a step: its share of the (sub-page, K or V) pairs
+  auto issue = [&](const Window &win, int ws, int buf) __attribute__((always_inline)) {
+#pragma unroll
+    for (int part = 0; part < C::LPW / C::LPS; ++part) {
+      // bf16: sub-page `wave` of K, then of V; fp32: sub-page wave % 2 of K or V
+      const int sub = C::SUBS == 4 ? wave : wave & 1;
+      const bool is_v = C::SUBS == 4 ? part == 1 : wave >= 2;
+      const int idx = ws * C::SUBS + sub;
+      const int page = __builtin_amdgcn_readlane(win.page, idx);
+      const int inf = __builtin_amdgcn_readlane(win.info, idx);
+      const int valid = (inf >> 8) & 31;
+      const char *src = (is_v ? vpool : kpool) +
+                        ((((int64_t)a.layer * pl.num_pages + page) * pl.Hkv + g) * pl.P +
+                         (inf & 255)) * (int64_t)C::ROW;
+      char *dst = lds + (is_v ? 2 * C::BUF : 0) + buf * C::BUF + sub * 16 * C::ROW;
+      int off[C::LPS];
+#pragma unroll
+      for (int c = 0; c < C::LPS; ++c) {
+        const int byte = 1024 * c + 16 * lane;
+        const int r = byte / C::ROW, x = byte % C::ROW / 16;      // x: where it lands
+        off[c] = r * C::ROW + 16 * (is_v ? v_piece<T, D>(r, x) : k_piece<T, D>(sub * 16 + r, x));
+      }
+      load_sub_page(src, valid * C::ROW, dst, off);
+    }
+  };
+
+  f32x16 o[C::DT];
+  float ref, l;            // reference max in log2 units (-inf: no key yet), sum of this half
+  bool careful = false;    // second run of a unit whose outputs were not all finite
+  while (true) {
+#pragma unroll
+    for (int d = 0; d < C::DT; ++d)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) o[d][r] = 0.0f;
+    ref = -INFINITY;
+    l = 0.0f;
+    bool all_set = false, masked = false;
+    Window win = fill(0), nxt = win;
+    if (steps > 0) issue(win, 0, 0);
+    for (int st = 0; st < steps; ++st) {
+      const int ws = st % WSTEPS;
+      const int buf = careful ? 0 : st & 1;
+      if (ws == 0 && st + WSTEPS < steps) nxt = fill((st + WSTEPS) * C::SUBS);
+      // this step's loads have landed, and every wave is done with the other buffer
+      __builtin_amdgcn_s_waitcnt(0);
+      __syncthreads();
+      const Window cur = win;
+      if (ws == WSTEPS - 1) win = nxt;
+      if (!careful && st + 1 < steps) issue(win, (st + 1) % WSTEPS, buf ^ 1);
+      int flags = 0, none = kNone;
+#pragma unroll
+      for (int sb = 0; sb < C::SUBS; ++sb) {
+        const int inf = __builtin_amdgcn_readlane(cur.info, ws * C::SUBS + sb);
+        flags |= inf;
+        none &= inf;
+      }
+      if (any_live && !none) {
+        // S^T: lane = row, register 4 j + i of tile kt = key 32 kt + 8 j + 4 h + i
+        const char *kb = lds + buf * C::BUF;
+        f32x16 s[C::NS];
+#pragma unroll
+        for (int kt = 0; kt < C::NS; ++kt) {
+#pragma unroll
+          for (int r = 0; r < 16; ++r) s[kt][r] = 0.0f;
+          const int key = 32 * kt + lr;
+#pragma unroll
+          for (int i = 0; i < C::NQ; ++i) {
+            const qvec kf = *reinterpret_cast<const qvec *>(
+                kb + key * C::ROW + k_piece<T, D>(key, 2 * i + h) * 16);
+            if constexpr (sizeof(T) == 2) {
+              s[kt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[i], s[kt], 0, 0, 0);
+            } else {
+#pragma unroll
+              for (int e = 0; e < 4; ++e)
+                s[kt] = __builtin_amdgcn_mfma_f32_32x32x2f32(kf[e], qf[i][e], s[kt], 0, 0, 0);
+            }
+          }
+        }
+        bool move = !all_set;
+        uint32_t hidden = 0;                 // careful run: registers of S not to be seen
+        const bool mask = (flags & (kMask | kNone)) != 0;
+        if (mask) {
+          masked = move = true;
+#pragma unroll
+          for (int sb = 0; sb < C::SUBS; ++sb) {
+            const int idx = ws * C::SUBS + sb;
+            const int inf = __builtin_amdgcn_readlane(cur.info, idx);
+            const int ei = __builtin_amdgcn_readlane(cur.ent, idx);
+            const int slot = __builtin_amdgcn_readlane(cur.slot, idx);
+            const int valid = (inf >> 8) & 31;          // 0 beyond the unit's end
+            const Entry *en = ents_lds ? &sh_ent[ei] : &ents[ei];
+            int lim = 0;
+            if (en->own & seq_bit) lim = qslot + 1 - slot;
+            else if (en->below & seq_bit) lim = 16;
+            lim = live ? min(lim, valid) : valid;
+#pragma unroll
+            for (int j = 0; j < 2; ++j)
+#pragma unroll
+              for (int i = 0; i < 4; ++i)
+                if (8 * j + 4 * h + i >= lim) {
+                  s[sb / 2][8 * (sb & 1) + 4 * j + i] = -INFINITY;
+                  if (careful) hidden |= 1u << (8 * sb + 4 * j + i);
+                }
+          }
+        }
+        float p[C::NS][16], sum;
+        auto terms = [&](float r) __attribute__((always_inline)) {
+          float part[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+          for (int kt = 0; kt < C::NS; ++kt)
+#pragma unroll
+            for (int x = 0; x < 16; ++x) {
+              p[kt][x] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[kt][x], a.sl2, -r));
+              part[x & 3] += p[kt][x];
+            }
+          sum = (part[0] + part[1]) + (part[2] + part[3]);
+        };
+        if (!move) {
+          terms(ref);
+          move = ballot(!(sum < kMoveAt)) != 0;
+        }
+        if (move) {
+          float mx = -INFINITY;
+#pragma unroll
+          for (int kt = 0; kt < C::NS; ++kt)
+#pragma unroll
+            for (int x = 0; x < 16; ++x) mx = fmaxf(mx, s[kt][x]);
+          mx = swap_halves_max(mx) * a.sl2;
+          const float to = fmaxf(ref, mx);
+          const float by = to == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(ref - to);
+          l *= by;
+#pragma unroll
+          for (int d = 0; d < C::DT; ++d)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) o[d][r] *= by;
+          ref = to;
+          terms(to == -INFINITY ? 0.0f : to);
+          if (!mask) all_set = true;
+        }
+        l += sum;
+        // O^T += V^T P^T
+        const char *vb = lds + 2 * C::BUF + buf * C::BUF;
+        if (!careful) {
+          if constexpr (sizeof(T) == 2) {
+            // two transposing reads give the lane's column 32 d + lr of the keys
+            // 16 ks + 4 h + i and 16 ks + 8 + 4 h + i, the order that P has: lane x of
+            // 16 addresses four columns from 4 (x % 4) of key x / 4
+            const int x16 = lane & 15, col = ((lane >> 4) & 1) * 16 + 4 * (x16 & 3);
+#pragma unroll
+            for (int ks = 0; ks < C::KEYS / 16; ++ks) {
+              bf16x8 pf;
+#pragma unroll
+              for (int e = 0; e < 8; ++e) pf[e] = (__bf16)p[ks / 2][8 * (ks & 1) + e];
+#pragma unroll
+              for (int d = 0; d < C::DT; ++d) {
+                bf16x4 v2[2];
+#pragma unroll
+                for (int y = 0; y < 2; ++y) {
+                  const int key = 16 * ks + 8 * y + 4 * h + (x16 >> 2);
+                  const int c = 32 * d + col;
+                  typedef short s16x4 __attribute__((ext_vector_type(4)));
+                  typedef __attribute__((address_space(3))) s16x4 *P4;
+                  const s16x4 tv = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                      (P4)(vb + key * C::ROW + v_piece<T, D>(key & 15, c / 8) * 16 + c % 8 * 2));
+                  v2[y] = __builtin_bit_cast(bf16x4, tv);
+                }
+                const bf16x8 vf = __builtin_shufflevector(v2[0], v2[1], 0, 1, 2, 3, 4, 5, 6, 7);
+                o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, pf, o[d], 0, 0, 0);
+              }
+            }
+          } else {
+#pragma unroll
+            for (int x = 0; x < 16; ++x) {
+              const int key = 8 * (x / 4) + 4 * h + x % 4;
+#pragma unroll
+              for (int d = 0; d < C::DT; ++d) {
+                const int c = 32 * d + lr;
+                const float vf = *reinterpret_cast<const float *>(
+                    vb + key * C::ROW + v_piece<T, D>(key & 15, c / 4) * 16 + c % 4 * 4);
+                o[d] = __builtin_amdgcn_mfma_f32_32x32x2f32(vf, p[0][x], o[d], 0, 0, 0);
+              }
+            }
+          }
+        } else {
+          // A key that a row may not see has p = 0, but 0 times an infinite or NaN
+          // value is not 0: here it is left out (marked by -1).  16 keys of P at a time
+          // go through the buffer that a careful run does not load into.
+          float *scr = reinterpret_cast<float *>(lds + C::BUF) + wave * 512;
+#pragma unroll
+          for (int ks = 0; ks < C::KEYS / 16; ++ks) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+              scr[(8 * (e / 4) + 4 * h + e % 4) * 32 + lr] =
+                  hidden >> (8 * ks + e) & 1 ? -1.0f : p[ks / 2][8 * (ks & 1) + e];
+            __builtin_amdgcn_s_waitcnt(0);
+            __builtin_amdgcn_wave_barrier();
+            for (int key = 0; key < 16; ++key) {
+              const float pk = scr[key * 32 + lr];
+              const char *vr = vb + (16 * ks + key) * C::ROW;
+#pragma unroll
+              for (int d = 0; d < C::DT; ++d)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) {
+                  const int c = 32 * d + 8 * (r / 4) + 4 * h + r % 4;
+                  const float vv = (float)*reinterpret_cast<const T *>(
+                      vr + v_piece<T, D>(key, c * C::ES / 16) * 16 + c * C::ES % 16);
+                  if (!(pk < 0.0f)) o[d][r] += pk * vv;
+                }
+            }
+            __builtin_amdgcn_wave_barrier();
+          }
+        }
+      }
+      if (careful && st + 1 < steps) {
+        __syncthreads();                       // every wave is done with the one buffer
+        issue(win, (st + 1) % WSTEPS, 0);
+      }
+    }
+    if (careful) break;
+    bool finite = true;
+#pragma unroll
+    for (int d = 0; d < C::DT; ++d)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) finite = finite && __builtin_isfinite(o[d][r]);
+    if (!__syncthreads_or(live && masked && !finite)) break;
+    careful = true;
+  }
+  if (ballot(stale)) {
+    if (lane == 0) status_error(a.status, ARBOR_EINVAL);
+    return;
+  }
+  const float lt = swap_halves_add(l);
+  if (!live) return;
+  if (un.part >= 0) {
+    if (un.part >= a.part_cap) return;         // (the plan's bound holds)
+    float *pp = a.part + (((int64_t)un.part * pl.Hkv + g) * kRows + row) * (D + 4);
+#pragma unroll
+    for (int d = 0; d < C::DT; ++d)
+#pragma unroll
+      for (int r = 0; r < 16; r += 4)
+        *reinterpret_cast<f32x4 *>(pp + 32 * d + 2 * r + 4 * h) =
+            f32x4{o[d][r], o[d][r + 1], o[d][r + 2], o[d][r + 3]};
+    if (h == 0) {
+      pp[D] = ref;
+      pp[D + 1] = lt;
+    }
+    return;
+  }
+  const float inv = lt == 0.0f ? 0.0f : 1.0f / lt;
+  T *op = static_cast<T *>(a.out) + ((int64_t)tok * Hq + head) * D;
+  typedef T ovec __attribute__((ext_vector_type(4)));
+#pragma unroll
+  for (int d = 0; d < C::DT; ++d)
+#pragma unroll
+    for (int r = 0; r < 16; r += 4) {
+      ovec w;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) w[i] = (T)(o[d][r + i] * inv);
+      *reinterpret_cast<ovec *>(op + 32 * d + 2 * r + 4 * h) = w;
+    }
+  if (a.lse && h == 0) {
+    const float rf = ref == -INFINITY && lt != 0.0f ? 0.0f : ref;
+    a.lse[(int64_t)tok * Hq + head] = (rf + __builtin_amdgcn_logf(lt)) * kLn2;
+  }
+}
+
+// Joins the parts of the tiles that have several: a workgroup per 16 rows of a tile
+// and KV head, D / 4 lanes a row, parts in order.
+template <class T, int D>
+__global__ __launch_bounds__(256) void prefill_join(AttnArgs a) {
+  if (status_failed(a.status) || !header_ok(a)) return;
+  constexpr int LPR = D / 4, RPW = 256 / LPR, NG = kRows / RPW;
+  const Pool &pl = a.pl;
+  int x = blockIdx.x;
+  const int grp = x % NG;
+  x /= NG;
+  const int g = x % pl.Hkv, k = x / pl.Hkv;
+  if (k >= a.p.head->n_split) return;
+  const Tile tl = a.p.tiles[a.p.split[k]];
+  const int row = grp * RPW + threadIdx.x / LPR, c = threadIdx.x % LPR * 4;
+  const int tq = row / pl.G;
+  if (tq >= tl.nt || tl.part0 + tl.parts > a.part_cap) return;
+  const int64_t stride = (int64_t)pl.Hkv * kRows * (D + 4);
+  const float *pp = a.part + (((int64_t)tl.part0 * pl.Hkv + g) * kRows + row) * (D + 4);
+  float m = -INFINITY;
+  for (int e = 0; e < tl.parts; ++e) m = fmaxf(m, pp[e * stride + D]);
+  const float base = m == -INFINITY ? 0.0f : m;
+  float l = 0.0f;
+  f32x4 o = {0.0f, 0.0f, 0.0f, 0.0f};
+  for (int e = 0; e < tl.parts; ++e) {
+    const float *q = pp + e * stride;
+    const float ref = q[D];
+    // a part whose terms have no reference holds sums of 0 (or NaN, which stays)
+    const float w = ref == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(ref - base);
+    l += w * q[D + 1];
+    const f32x4 v = *reinterpret_cast<const f32x4 *>(q + c);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) o[i] += w * v[i];
+  }
+  const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+  const int Hq = pl.Hkv * pl.G, head = g * pl.G + row - tq * pl.G;
+  const int64_t tok = tl.t0 + tq;
+  typedef T ovec __attribute__((ext_vector_type(4)));
+  ovec w;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) w[i] = (T)(o[i] * inv);
+  *reinterpret_cast<ovec *>(static_cast<T *>(a.out) + (tok * Hq + head) * D + c) = w;
+  if (a.lse && c == 0)
+    a.lse[tok * Hq + head] = ((m == -INFINITY && l != 0.0f ? 0.0f : m) +
+                              __builtin_amdgcn_logf(l)) * kLn2;
+}
+
+inline int64_t part_bound(const arbor_geom_t *g, int n_seq, int n_tokens) {
+  // a tile in np parts has more than (np - 1) of an even share; np <= 2 (np - 1)
+  (void)n_seq;
+  (void)n_tokens;
+  return 2 * (int64_t)target_parts(g->num_kv_heads);
+}
+
+inline size_t part_floats(const arbor_geom_t *g) {
+  return (size_t)g->num_kv_heads * kRows * (g->head_dim + 4);
+}
+
+}  // namespace
+
+size_t prefill_plan_size(const arbor_geom_t *g, int32_t n_seq, int32_t n_tokens) {
+  size_t need = 0;
+  (void)carve_plan(g, n_seq, n_tokens, nullptr, 0, &need);
+  return need + 256;
+}
+
+size_t prefill_workspace_size(const arbor_geom_t *g, int32_t n_seq, int32_t n_tokens) {
+  if (n_tokens == 0) return 256;
+  return (size_t)part_bound(g, n_seq, n_tokens) * part_floats(g) * 4 + 256;
+}
+
+int launch_prefill_plan(const arbor_geom_t *geom, const arbor_tree_t *tree, const int32_t *nodes,
+                        int32_t n_seq, const int32_t *cu, int32_t n_tokens, void *plan,
+                        size_t plan_bytes, int32_t *status, hipStream_t stream) {
+  if (n_tokens == 0 || n_seq == 0) return ARBOR_OK;
+  const PlanPtrs p = carve_plan(geom, n_seq, n_tokens, plan, plan_bytes, nullptr);
+  if (!p.head) return ARBOR_EWORKSPACE;
+  const Tree t = make_tree(tree);
+  hipLaunchKernelGGL(plan_tiles, dim3(1), dim3(1024), 0, stream, t, geom->q_per_kv,
+                     geom->num_kv_heads, geom->page_size, nodes, n_seq, cu, n_tokens, p, status);
+  hipLaunchKernelGGL(plan_chains, dim3((unsigned)p.tiles_cap), dim3(64), 0, stream, t, nodes, cu, p,
+                     status);
+  hipLaunchKernelGGL(plan_units, dim3(1), dim3(1024), 0, stream, p,
+                     target_parts(geom->num_kv_heads), status);
+  return hip_ok(hipGetLastError());
+}
+
+int launch_prefill(const arbor_geom_t *geom, const arbor_tree_t *tree, const arbor_pool_t *pool,
+                   const void *plan, size_t plan_bytes, int32_t n_seq, int32_t n_tokens,
+                   int32_t layer, const void *q, void *out, float *lse, float softmax_scale,
+                   int32_t *status, void *workspace, size_t workspace_bytes, hipStream_t stream) {
+  if (n_tokens == 0 || n_seq == 0) return ARBOR_OK;
+  AttnArgs a;
+  a.p = carve_plan(geom, n_seq, n_tokens, const_cast<void *>(plan), plan_bytes, nullptr);
+  if (!a.p.head) return ARBOR_EWORKSPACE;
+  Carve cv(workspace, workspace_bytes);
+  a.part_cap = part_bound(geom, n_seq, n_tokens);
+  a.part = cv.take<float>((size_t)a.part_cap * part_floats(geom));
+  if (!cv.ok) return ARBOR_EWORKSPACE;
+  a.t = make_tree(tree);
+  a.pl = make_pool(geom, pool);
+  a.n_seq = n_seq;
+  a.n_tokens = n_tokens;
+  a.layer = layer;
+  a.q = q;
+  a.out = out;
+  a.lse = lse;
+  a.sl2 = (softmax_scale > 0.0f ? softmax_scale : 1.0f / sqrtf((float)geom->head_dim)) * kLog2e;
+  a.status = status;
+  const int target = target_parts(geom->num_kv_heads);
+  const int64_t units = a.p.units_cap * geom->num_kv_heads;
+  const int64_t tiles = a.p.tiles_cap < target ? a.p.tiles_cap : target;
+  if (units > INT32_MAX) return ARBOR_EUNSUPPORTED;
+#define ARBOR_PREFILL_LAUNCH(T, D)                                                             \
+  do {                                                                                         \
+    timing_begin(geom, ARBOR_KERNEL_PREFILL_ATTN, stream);                                     \
+    hipLaunchKernelGGL((prefill_attn<T, D>), dim3((unsigned)units), dim3(kRows * 2),           \
+                       (Cfg<T, D>::LDS), stream, a);                                           \
+    timing_end(geom, ARBOR_KERNEL_PREFILL_ATTN, stream);                                       \
+    hipLaunchKernelGGL((prefill_join<T, D>),                                                   \
+                       dim3((unsigned)(tiles * geom->num_kv_heads * (kRows * D / 4 / 256))),   \
+                       dim3(256), 0, stream, a);                                               \
+  } while (0)
+  if (geom->dtype == ARBOR_BF16) {
+    if (geom->head_dim == 128) ARBOR_PREFILL_LAUNCH(__bf16, 128);
+    else ARBOR_PREFILL_LAUNCH(__bf16, 64);
+  } else {
+    if (geom->head_dim == 128) ARBOR_PREFILL_LAUNCH(float, 128);
+    else ARBOR_PREFILL_LAUNCH(float, 64);
+  }
+#undef ARBOR_PREFILL_LAUNCH
+  return hip_ok(hipGetLastError());
+}
+
+}  // namespace arbor
