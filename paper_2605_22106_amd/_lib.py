@@ -212,6 +212,10 @@ class KVState:
     dtype: int
     num_tokens: int
 
+    def __setattr__(self, name, value):
+        self.__dict__.pop("_built", None)       # see _descriptors
+        self.__dict__[name] = value
+
     @property
     def num_nodes(self) -> int:
         return int(self.parent.numel())
@@ -438,28 +442,59 @@ def arbor_uncertainty(logits, top_k, u_out, status, workspace, dst=None, stream=
 
 
 # ---- growing the tree ---------------------------------------------------------
-# These check shapes and types too: the packed rows' counts are taken from them.
+# A layer of a model is a few microseconds of kernels for a few new tokens, so these
+# calls spend little on the host: the descriptors of a KVState are built once for the
+# tensors that it holds, pointers go over as integers, and one comparison of the device
+# stands for "on the GPU" and "on the current device".  They check shapes and types:
+# the packed rows' counts are taken from them.
 
-def _is(t, name: str, dtype, *shape):
-    """Pointer of a contiguous GPU tensor of this type and shape, on the current device."""
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+
+
+def _stream_of(stream, device: int) -> int:
+    if stream is not None:
+        return stream.cuda_stream
+    return _raw_stream(device) if _raw_stream else torch.cuda.current_stream().cuda_stream
+
+
+def _descriptors(kv: KVState):
+    """(device, geometry, tree, pool, n_full) of kv's tensors for a call; built again when a
+    field of kv has been set, or one of its tensors been moved or resized in place."""
+    now = (kv.parent.numel(), kv.k.numel(), kv.parent.data_ptr(), kv.n_full.data_ptr(), kv.tok_off.data_ptr(),
+           kv.page_off.data_ptr(), kv.n_kept.data_ptr(), kv.page_table.data_ptr(),
+           kv.k.data_ptr(), kv.v.data_ptr(), kv.slot_pos.data_ptr(), kv.free_stack.data_ptr(),
+           kv.free_top.data_ptr())
+    d = kv.__dict__.get("_built")
+    if d is None or d[0] != now:
+        g, t, p = kv.geom(), kv.tree(), kv.pool()
+        d = (now, kv.k.get_device(), ctypes.byref(g), ctypes.byref(t), ctypes.byref(p))
+        kv.__dict__["_built"] = d
+    if d[1] != torch.cuda.current_device():
+        raise ValueError("the tree and pool must be on the current device")
+    return d[1:] + (now[3],)
+
+
+def _is(t, name: str, dtype, shape: tuple, device: int):
+    """Pointer of a contiguous tensor of this type and shape on this device."""
     if t is None:
         return None
-    if t.dtype != dtype or tuple(t.shape) != tuple(shape):
-        raise ValueError(f"{name} must be {dtype} of shape {tuple(shape)}, "
-                         f"not {t.dtype} of shape {tuple(t.shape)}")
-    p = _dev(t, name)
-    if t.device.index != torch.cuda.current_device():
-        raise ValueError(f"{name} must be on the current device")
-    return p
+    if (t.dtype is not dtype or t.shape != shape or t.get_device() != device or device < 0 or
+            not t.is_contiguous()):
+        raise ValueError(f"{name} must be a contiguous {dtype} GPU tensor of shape {shape} on the "
+                         f"current device, not {t.dtype} of shape {tuple(t.shape)} on {t.device}")
+    return t.data_ptr()
 
 
-def _element(kv: KVState):
-    return torch.bfloat16 if kv.dtype == BF16 else torch.float32
+def _bytes(t, name: str, device: int):
+    """Pointer and size of a workspace or plan (uint8)."""
+    n = t.numel()
+    return _is(t, name, torch.uint8, (n,), device), n
 
 
-def _packed(nodes, cu):
-    n_seq = int(nodes.numel())
-    return n_seq, _is(nodes, "nodes", torch.int32, n_seq), _is(cu, "cu", torch.int32, n_seq + 1)
+def _packed(nodes, cu, device: int):
+    n_seq = nodes.numel()
+    return (n_seq, _is(nodes, "nodes", torch.int32, (n_seq,), device),
+            _is(cu, "cu", torch.int32, (n_seq + 1,), device))
 
 
 def arbor_extend(kv: KVState, nodes, cu, slots, positions, tokens, status, workspace,
@@ -467,56 +502,63 @@ def arbor_extend(kv: KVState, nodes, cu, slots, positions, tokens, status, works
     """Reserve slots for the packed tokens cu[e] .. cu[e+1] of block nodes[e]
     (ascending); the rows of `slots` (int64), `positions` (int32) and `tokens`
     (int64 or None) are the packed rows."""
-    g, t, p = kv.geom(), kv.tree(), kv.pool()
-    n_seq, nd, c = _packed(nodes, cu)
-    n = int(slots.numel())
-    return load().arbor_extend(ctypes.byref(g), ctypes.byref(t), ctypes.byref(p),
-                               _dev(kv.n_full, "n_full"), nd, n_seq, c, n,
-                               _is(slots, "slots", torch.int64, n),
-                               _is(positions, "positions", torch.int32, n),
-                               _is(tokens, "tokens", torch.int64, n),
-                               _is(status, "status", torch.int32, 1),
-                               _dev(workspace, "workspace"), int(workspace.numel()),
-                               _stream(stream))
+    dev, g, t, p, n_full = _descriptors(kv)
+    n_seq, nd, c = _packed(nodes, cu, dev)
+    n = slots.numel()
+    ws, size = _bytes(workspace, "workspace", dev)
+    return load().arbor_extend(g, t, p, n_full, nd, n_seq, c, n,
+                               _is(slots, "slots", torch.int64, (n,), dev),
+                               _is(positions, "positions", torch.int32, (n,), dev),
+                               _is(tokens, "tokens", torch.int64, (n,), dev),
+                               _is(status, "status", torch.int32, (1,), dev), ws, size,
+                               _stream_of(stream, dev))
 
 
 def arbor_truncate(kv: KVState, nodes, keep, status, workspace, stream=None) -> int:
     """Block nodes[e] (ascending) keeps its tokens at positions below keep[e]."""
-    g, t, p = kv.geom(), kv.tree(), kv.pool()
-    n = int(nodes.numel())
-    return load().arbor_truncate(ctypes.byref(g), ctypes.byref(t), ctypes.byref(p),
-                                 _dev(kv.n_full, "n_full"), _is(nodes, "nodes", torch.int32, n),
-                                 _is(keep, "keep", torch.int32, n), n,
-                                 _is(status, "status", torch.int32, 1),
-                                 _dev(workspace, "workspace"), int(workspace.numel()),
-                                 _stream(stream))
+    dev, g, t, p, n_full = _descriptors(kv)
+    n = nodes.numel()
+    ws, size = _bytes(workspace, "workspace", dev)
+    return load().arbor_truncate(g, t, p, n_full, _is(nodes, "nodes", torch.int32, (n,), dev),
+                                 _is(keep, "keep", torch.int32, (n,), dev), n,
+                                 _is(status, "status", torch.int32, (1,), dev), ws, size,
+                                 _stream_of(stream, dev))
 
 
 def arbor_fork(kv: KVState, src, dst, status, workspace, A=None, rows_seen=None,
                stream=None) -> int:
     """The empty block dst[e] (ascending) becomes a copy of block src[e]."""
-    g, t, p = kv.geom(), kv.tree(), kv.pool()
-    n = int(dst.numel())
-    return load().arbor_fork(ctypes.byref(g), ctypes.byref(t), ctypes.byref(p),
-                             _dev(kv.n_full, "n_full"), _is(src, "src", torch.int32, n),
-                             _is(dst, "dst", torch.int32, n), n,
-                             _is(A, "A", torch.float32, kv.num_tokens),
-                             _is(rows_seen, "rows_seen", torch.int64, kv.num_nodes),
-                             _is(status, "status", torch.int32, 1), _dev(workspace, "workspace"),
-                             int(workspace.numel()), _stream(stream))
+    dev, g, t, p, n_full = _descriptors(kv)
+    n = dst.numel()
+    ws, size = _bytes(workspace, "workspace", dev)
+    return load().arbor_fork(g, t, p, n_full, _is(src, "src", torch.int32, (n,), dev),
+                             _is(dst, "dst", torch.int32, (n,), dev), n,
+                             _is(A, "A", torch.float32, (kv.num_tokens,), dev),
+                             _is(rows_seen, "rows_seen", torch.int64, (kv.num_nodes,), dev),
+                             _is(status, "status", torch.int32, (1,), dev), ws, size,
+                             _stream_of(stream, dev))
 
 
-def _rows(x, name: str, dtype, n: int, width: int):
+def _rows(x, name: str, dtype, n: int, width: int, device: int):
     """Pointer and row stride of n rows of `width` elements side by side; [n, width] or
     [n, heads, head_dim], where rows may lie further apart than they are long."""
-    if x.dtype != dtype or x.dim() not in (2, 3) or x.shape[0] != n or x[:1].numel() != (
-            width if n else 0):
-        raise ValueError(f"{name} must be {dtype} rows [{n}, {width}]")
-    if not x.is_cuda or x.device.index != torch.cuda.current_device():
-        raise ValueError(f"{name} must be a GPU tensor on the current device")
-    if x.stride(-1) != 1 or (x.dim() == 3 and x.stride(1) != x.shape[2]):
-        raise ValueError(f"the elements of a row of {name} must be contiguous")
-    return ctypes.c_void_p(x.data_ptr()), int(x.stride(0)) if n > 1 else width
+    shape, stride = x.shape, x.stride()
+    flat = len(shape) == 2
+    if (x.dtype is not dtype or x.get_device() != device or device < 0 or not 2 <= len(shape) <= 3
+            or shape[0] != n or (shape[1] if flat else shape[1] * shape[2]) != width
+            or stride[-1] != 1 or not (flat or stride[1] == shape[2])):
+        raise ValueError(f"{name} must be {dtype} rows [{n}, {width}] on the current device, each "
+                         f"of them contiguous, not {x.dtype} of shape {tuple(shape)} and strides "
+                         f"{stride} on {x.device}")
+    return x.data_ptr(), stride[0] if n > 1 else width
+
+
+def _record(x, name: str, dtype, shape: tuple):
+    if x is None:
+        return None
+    if x.dtype is not dtype or x.shape != shape:
+        raise ValueError(f"{name} must be {dtype} of shape {shape}")
+    return _host_or_dev(x, name).value
 
 
 def arbor_append(kv: KVState, layer, q, k, v, slots, positions, q_out, status, q_norm=None,
@@ -525,27 +567,26 @@ def arbor_append(kv: KVState, layer, q, k, v, slots, positions, q_out, status, q
     """Norm and rotate the queries and keys of packed tokens (rows of q, k, v, which
     may be slices of one product's rows), and write keys and values to `slots` of
     layer `layer`; rotary_dim is twice the length of inv_freq (fp32)."""
-    g, t, p = kv.geom(), kv.tree(), kv.pool()
-    n, d, dt = int(slots.numel()), kv.head_dim, _element(kv)
-    hq = kv.kv_heads * kv.q_per_kv
-    qp, qs = _rows(q, "q", dt, n, hq * d)
-    kp, ks = _rows(k, "k", dt, n, kv.kv_heads * d)
-    vp, vs = _rows(v, "v", dt, n, kv.kv_heads * d)
-    rec = []
-    for x, name in ((record_k, "record_k"), (record_v, "record_v")):
-        if x is not None and (x.dtype != dt or tuple(x.shape) != (kv.num_tokens, kv.layers,
-                                                                  kv.kv_heads, d)):
-            raise ValueError(f"{name} must be {dt} [num_tokens, layers, kv_heads, head_dim]")
-        rec.append(None if x is None else _host_or_dev(x, name))
-    half = 0 if inv_freq is None else int(inv_freq.numel())
-    a = Append(qp, kp, vp, qs, ks, vs, _is(q_norm, "q_norm", dt, d), _is(k_norm, "k_norm", dt, d),
-               _is(inv_freq, "inv_freq", torch.float32, half), _is(slots, "slots", torch.int64, n),
-               _is(positions, "positions", torch.int32, n),
-               _is(tokens, "tokens", torch.int64, n), rec[0], rec[1],
-               _is(q_out, "q_out", dt, n, hq, d), float(eps), 2 * half, int(bool(interleaved)))
-    return load().arbor_append(ctypes.byref(g), ctypes.byref(t), ctypes.byref(p), int(layer),
-                               ctypes.byref(a), n, _is(status, "status", torch.int32, 1),
-                               _stream(stream))
+    dev, g, t, p, _ = _descriptors(kv)
+    n, d, heads = slots.numel(), kv.head_dim, kv.kv_heads
+    dt = torch.bfloat16 if kv.dtype == BF16 else torch.float32
+    hq = heads * kv.q_per_kv
+    qp, qs = _rows(q, "q", dt, n, hq * d, dev)
+    kp, ks = _rows(k, "k", dt, n, heads * d, dev)
+    vp, vs = _rows(v, "v", dt, n, heads * d, dev)
+    rec = (kv.num_tokens, kv.layers, heads, d)
+    half = 0 if inv_freq is None else inv_freq.numel()
+    a = Append(qp, kp, vp, qs, ks, vs, _is(q_norm, "q_norm", dt, (d,), dev),
+               _is(k_norm, "k_norm", dt, (d,), dev),
+               _is(inv_freq, "inv_freq", torch.float32, (half,), dev),
+               _is(slots, "slots", torch.int64, (n,), dev),
+               _is(positions, "positions", torch.int32, (n,), dev),
+               _is(tokens, "tokens", torch.int64, (n,), dev),
+               _record(record_k, "record_k", dt, rec), _record(record_v, "record_v", dt, rec),
+               _is(q_out, "q_out", dt, (n, hq, d), dev), eps, 2 * half, bool(interleaved))
+    return load().arbor_append(g, t, p, layer, ctypes.byref(a), n,
+                               _is(status, "status", torch.int32, (1,), dev),
+                               _stream_of(stream, dev))
 
 
 def arbor_prefill_plan_size(kv: KVState, n_seq: int, n_tokens: int) -> int:
@@ -561,25 +602,30 @@ def arbor_prefill_workspace_size(kv: KVState, n_seq: int, n_tokens: int) -> int:
 def arbor_prefill_plan(kv: KVState, nodes, cu, n_tokens, plan, status, stream=None) -> int:
     """The work list of arbor_tree_prefill_attn for the newest tokens of blocks, into
     `plan` (arbor_prefill_plan_size bytes)."""
-    g, t = kv.geom(), kv.tree()
-    n_seq, nd, c = _packed(nodes, cu)
-    return load().arbor_prefill_plan(ctypes.byref(g), ctypes.byref(t), nd, n_seq, c, int(n_tokens),
-                                     _dev(plan, "plan"), int(plan.numel()),
-                                     _is(status, "status", torch.int32, 1), _stream(stream))
+    dev, g, t, _, _ = _descriptors(kv)
+    n_seq, nd, c = _packed(nodes, cu, dev)
+    pp, size = _bytes(plan, "plan", dev)
+    return load().arbor_prefill_plan(g, t, nd, n_seq, c, n_tokens, pp, size,
+                                     _is(status, "status", torch.int32, (1,), dev),
+                                     _stream_of(stream, dev))
 
 
 def arbor_tree_prefill_attn(kv: KVState, plan, n_seq, layer, q, out, lse_out, softmax_scale,
                             status, workspace, stream=None, timing=None) -> int:
     """Causal attention of the packed tokens q [n_tokens, Hq, head_dim] over their
     chains, by the plan made for them."""
-    g, t, p = kv.geom(timing), kv.tree(), kv.pool()
-    n, hq, dt = int(q.shape[0]), kv.kv_heads * kv.q_per_kv, _element(kv)
-    return load().arbor_tree_prefill_attn(ctypes.byref(g), ctypes.byref(t), ctypes.byref(p),
-                                          _dev(plan, "plan"), int(plan.numel()), int(n_seq), n,
-                                          int(layer), _is(q, "q", dt, n, hq, kv.head_dim),
-                                          _is(out, "out", dt, n, hq, kv.head_dim),
-                                          _is(lse_out, "lse_out", torch.float32, n, hq),
-                                          float(softmax_scale),
-                                          _is(status, "status", torch.int32, 1),
-                                          _dev(workspace, "workspace"), int(workspace.numel()),
-                                          _stream(stream))
+    dev, g, t, p, _ = _descriptors(kv)
+    if timing is not None:
+        g = ctypes.byref(kv.geom(timing))
+    n, hq = q.shape[0], kv.kv_heads * kv.q_per_kv
+    dt = torch.bfloat16 if kv.dtype == BF16 else torch.float32
+    rows = (n, hq, kv.head_dim)
+    pp, plan_size = _bytes(plan, "plan", dev)
+    ws, size = _bytes(workspace, "workspace", dev)
+    return load().arbor_tree_prefill_attn(g, t, p, pp, plan_size, n_seq, n, layer,
+                                          _is(q, "q", dt, rows, dev),
+                                          _is(out, "out", dt, rows, dev),
+                                          _is(lse_out, "lse_out", torch.float32, (n, hq), dev),
+                                          softmax_scale,
+                                          _is(status, "status", torch.int32, (1,), dev), ws, size,
+                                          _stream_of(stream, dev))

@@ -365,6 +365,7 @@ struct Cfg {
   static constexpr int DT = D / 32;
   static constexpr int NQ = ROW / 32;                    // 16-byte operand pieces of a lane
   static constexpr int LDS = 4 * BUF;
+  static constexpr int PK = ES == 2 ? 16 : 2;            // keys of an MFMA of O
 };
 
 // Where piece x of row r of a step's K lies: rows 0..15 (of 16-lane groups that read
@@ -416,6 +417,34 @@ __host__ __device__ __forceinline__ void load_sub_page(const char *src, int byte
 #endif
 }
 
+// (the matrix instructions and the transposing read, host-device for the same reason)
+__host__ __device__ __forceinline__ f32x16 mfma_bf16(bf16x8 x, bf16x8 y, f32x16 c) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  return __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, y, c, 0, 0, 0);
+#else
+  return c;
+#endif
+}
+__host__ __device__ __forceinline__ f32x16 mfma_f32(float x, float y, f32x16 c) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  return __builtin_amdgcn_mfma_f32_32x32x2f32(x, y, c, 0, 0, 0);
+#else
+  return c;
+#endif
+}
+// Column of eight keys: four rows from p on and four from `next` bytes further on.
+__host__ __device__ __forceinline__ bf16x8 read_transposed(const char *p, int next) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  typedef short s16x4 __attribute__((ext_vector_type(4)));
+  typedef __attribute__((address_space(3))) s16x4 *P4;
+  const bf16x4 a = __builtin_bit_cast(bf16x4, __builtin_amdgcn_ds_read_tr16_b64_v4i16((P4)p));
+  const bf16x4 b = __builtin_bit_cast(bf16x4, __builtin_amdgcn_ds_read_tr16_b64_v4i16((P4)(p + next)));
+  return __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
+#else
+  return bf16x8{};
+#endif
+}
+
 __device__ __forceinline__ float swap_halves_add(float v) {
   float a, b;
   row_swap<true>(v, a, b);
@@ -429,10 +458,13 @@ __device__ __forceinline__ float swap_halves_max(float v) {
 
 // One sub-page per lane, 64 of them: read by readlane.
 struct Window {
-  int page, info, slot, ent;     // info: first row | valid rows << 8 | flags << 16
+  int page;
+  int info;      // first row of the page / 16 | valid rows << 8 | flags << 16
+  int place;     // chain block | first slot / 16 << 12
 };
 constexpr int kMask = 1 << 16;   // some row of this wave must not see some key of it
 constexpr int kNone = 1 << 17;   // no row of this wave sees any
+static_assert(kMaxSeq * MAXD <= 4096, "chain blocks of a tile fit 12 bits");
 
 __device__ __forceinline__ bool header_ok(const AttnArgs &a) {
   const Header *h = a.p.head;
@@ -455,12 +487,30 @@ __global__ __launch_bounds__(kRows * 2, 2) void prefill_attn(AttnArgs a) {
   if (u >= a.p.head->n_units) return;
   const Unit un = a.p.units[u];
   const Tile tl = a.p.tiles[un.tile];
-  const Entry *ents = a.p.ents + entry_base(un.tile, tl.e0);
+  // (global and LDS reads of a block stay apart: a pointer that may be either makes flat
+  // loads, which wait for both kinds)
+  typedef const __attribute__((address_space(1))) Entry *GlobalEnt;
+  const GlobalEnt ents = (GlobalEnt)(a.p.ents + entry_base(un.tile, tl.e0));
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int lr = lane & 31, h = lane >> 5;
   const bool ents_lds = tl.n_ent <= kEntLds;
-  for (int x = tid; x < tl.n_ent && ents_lds; x += kRows * 2) sh_ent[x] = ents[x];
+  auto entry = [&](int x) __attribute__((always_inline)) -> Entry {
+    Entry e;
+    if (ents_lds) {
+      e = sh_ent[x];
+    } else {
+      e.node = ents[x].node, e.limit = ents[x].limit, e.sub0 = ents[x].sub0, e.po = ents[x].po;
+      e.below = ents[x].below, e.own = ents[x].own;
+    }
+    return e;
+  };
+  for (int x = tid; x < tl.n_ent && ents_lds; x += kRows * 2) {
+    Entry e;
+    e.node = ents[x].node, e.limit = ents[x].limit, e.sub0 = ents[x].sub0, e.po = ents[x].po;
+    e.below = ents[x].below, e.own = ents[x].own;
+    sh_ent[x] = e;
+  }
   __syncthreads();
 
   // this lane's row
@@ -482,6 +532,7 @@ __global__ __launch_bounds__(kRows * 2, 2) void prefill_attn(AttnArgs a) {
   const int Hq = pl.Hkv * G;
   // Q as the B operand: its row, pieces 2 i + h
   typedef typename std::conditional<sizeof(T) == 2, bf16x8, f32x4>::type qvec;
+  typedef typename std::conditional<sizeof(T) == 2, bf16x8, float>::type pvec;
   qvec qf[C::NQ];
   {
     const T *qp = static_cast<const T *>(a.q) + ((int64_t)tok * Hq + head) * D;
@@ -493,25 +544,25 @@ __global__ __launch_bounds__(kRows * 2, 2) void prefill_attn(AttnArgs a) {
   const int n_sub = un.s1 - un.s0;
   const int steps = (n_sub + C::SUBS - 1) / C::SUBS;
   constexpr int WSTEPS = kWave / C::SUBS;         // steps of a window
+  static_assert(WSTEPS % 2 == 0, "a window ends with the second buffer");
   // sub-page w0 + lane of the unit
   bool stale = false;
-  auto fill = [&](int w0) -> Window {
+  auto fill = [&](int w0) __attribute__((always_inline)) -> Window {
     const int sp = un.s0 + w0 + lane;
-    Window w{0, kNone, 0, 0};
+    Window w{0, kNone, 0};
     if (sp >= un.s1) return w;
     int lo = 0, hi = tl.n_ent;
     while (hi - lo > 1) {
       const int mid = (lo + hi) / 2;
-      const int first = ents_lds ? sh_ent[mid].sub0 : ents[mid].sub0;
+      const int first = entry(mid).sub0;
       if (first <= sp) lo = mid;
       else hi = mid;
     }
     // (a block without a slot to see starts where the next one does: the last wins)
-    const Entry en = ents_lds ? sh_ent[lo] : ents[lo];
-    w.ent = lo;
-    w.slot = (sp - en.sub0) * 16;
-    int page = a.t.page_table[(int64_t)en.po + w.slot / pl.P];
-    const int valid = min(16, en.limit - w.slot);
+    const Entry en = entry(lo);
+    const int slot = (sp - en.sub0) * 16;
+    int page = a.t.page_table[(int64_t)en.po + slot / pl.P];
+    const int valid = min(16, en.limit - slot);
     if (page < 0 || page >= pl.num_pages) {       // the tree has changed since the plan
       stale = true;
       page = 0;
@@ -519,240 +570,261 @@ __global__ __launch_bounds__(kRows * 2, 2) void prefill_attn(AttnArgs a) {
     w.page = page;
     int flags = 0;
     const uint64_t mine = en.below & seqs, mown = en.own & seqs;
-    if (mine == 0 || (mine == mown && w.slot > qmax)) flags = kNone;
-    else if (mine != seqs || valid < 16 || (mown && w.slot + 15 > qmin)) flags = kMask;
-    w.info = w.slot % pl.P | valid << 8 | flags;
+    if (mine == 0 || (mine == mown && slot > qmax)) flags = kNone;
+    else if (mine != seqs || valid < 16 || (mown && slot + 15 > qmin)) flags = kMask;
+    w.info = slot % pl.P / 16 | valid << 8 | flags;
+    w.place = lo | slot / 16 << 12;
     return w;
   };
 
-  const char *kpool = static_cast<const char *>(pl.k);
-  const char *vpool = static_cast<const char *>(pl.v);
+  // the plane of this layer and head: pages are page_bytes apart
+  const int64_t page_bytes = (int64_t)pl.Hkv * pl.P * C::ROW;
+  const int64_t plane = (int64_t)a.layer * pl.num_pages * page_bytes + (int64_t)g * pl.P * C::ROW;
+  const char *kpool = static_cast<const char *>(pl.k) + plane;
+  const char *vpool = static_cast<const char *>(pl.v) + plane;
   // this wave's direct loads of a step: its share of the (sub-page, K or V) pairs
+  const int my_sub = C::SUBS == 4 ? wave : wave & 1;
+  int koff[C::LPS], voff[C::LPS];
+#pragma unroll
+  for (int c = 0; c < C::LPS; ++c) {
+    const int byte = 1024 * c + 16 * lane;
+    const int r = byte / C::ROW, x = byte % C::ROW / 16;      // x: the piece's place in LDS
+    koff[c] = r * C::ROW + 16 * k_piece<T, D>(my_sub * 16 + r, x);
+    voff[c] = r * C::ROW + 16 * v_piece<T, D>(r, x);
+  }
   auto issue = [&](const Window &win, int ws, int buf) __attribute__((always_inline)) {
-#pragma unroll
-    for (int part = 0; part < C::LPW / C::LPS; ++part) {
-      // bf16: sub-page `wave` of K, then of V; fp32: sub-page wave % 2 of K or V
-      const int sub = C::SUBS == 4 ? wave : wave & 1;
-      const bool is_v = C::SUBS == 4 ? part == 1 : wave >= 2;
-      const int idx = ws * C::SUBS + sub;
-      const int page = __builtin_amdgcn_readlane(win.page, idx);
-      const int inf = __builtin_amdgcn_readlane(win.info, idx);
-      const int valid = (inf >> 8) & 31;
-      const char *src = (is_v ? vpool : kpool) +
-                        ((((int64_t)a.layer * pl.num_pages + page) * pl.Hkv + g) * pl.P +
-                         (inf & 255)) * (int64_t)C::ROW;
-      char *dst = lds + (is_v ? 2 * C::BUF : 0) + buf * C::BUF + sub * 16 * C::ROW;
-      int off[C::LPS];
-#pragma unroll
-      for (int c = 0; c < C::LPS; ++c) {
-        const int byte = 1024 * c + 16 * lane;
-        const int r = byte / C::ROW, x = byte % C::ROW / 16;      // x: where it lands
-        off[c] = r * C::ROW + 16 * (is_v ? v_piece<T, D>(r, x) : k_piece<T, D>(sub * 16 + r, x));
-      }
-      load_sub_page(src, valid * C::ROW, dst, off);
-    }
+    const int idx = ws * C::SUBS + my_sub;
+    const int page = __builtin_amdgcn_readlane(win.page, idx);
+    const int inf = __builtin_amdgcn_readlane(win.info, idx);
+    const int64_t off = page * page_bytes + (inf & 255) * (16 * C::ROW);
+    const int bytes = (inf >> 8 & 31) * C::ROW;
+    char *dst = lds + buf * C::BUF + my_sub * 16 * C::ROW;
+    // bf16: sub-page `wave` of K and of V; fp32: sub-page wave % 2 of K or V
+    if (C::SUBS == 4 || wave < 2) load_sub_page(kpool + off, bytes, dst, koff);
+    if (C::SUBS == 4 || wave >= 2) load_sub_page(vpool + off, bytes, dst + 2 * C::BUF, voff);
   };
+
+  // this lane's operands in LDS: K row lr, pieces 2 i + h; V^T
+  int kat[C::NQ], vat[C::DT];
+#pragma unroll
+  for (int i = 0; i < C::NQ; ++i) kat[i] = lr * C::ROW + 16 * k_piece<T, D>(lr, 2 * i + h);
+#pragma unroll
+  for (int d = 0; d < C::DT; ++d) {
+    if constexpr (sizeof(T) == 2) {
+      // a transposing read of four keys: lane x of 16 addresses columns 4 (x % 4) .. of
+      // key x / 4 and gets column x of the four
+      const int x = lane & 15, key = 4 * h + (x >> 2), c = 32 * d + (lane & 16) + 4 * (x & 3);
+      vat[d] = key * C::ROW + 16 * v_piece<T, D>(key, c / 8) + c % 8 * 2;
+    } else {
+      const int c = 32 * d + lr;
+      vat[d] = 4 * h * C::ROW + 16 * v_piece<T, D>(4 * h, c / 4) + c % 4 * 4;
+    }
+  }
 
   f32x16 o[C::DT];
   float ref, l;            // reference max in log2 units (-inf: no key yet), sum of this half
-  bool careful = false;    // second run of a unit whose outputs were not all finite
-  while (true) {
+  bool all_set, masked;    // every row has a key; some key was hidden from some row
+
+  // One step: S^T, its terms, O^T.  CAREFUL: see below.
+  auto step = [&](const Window &cur, int ws, auto buf_c, auto careful_c)
+                  __attribute__((always_inline)) {
+    constexpr int BUF = decltype(buf_c)::value;
+    constexpr bool CAREFUL = decltype(careful_c)::value;
+    const char *kb = lds + BUF * C::BUF, *vb = lds + (2 + BUF) * C::BUF;
+    int flags = 0, none = kNone;
+#pragma unroll
+    for (int sb = 0; sb < C::SUBS; ++sb) {
+      const int inf = __builtin_amdgcn_readlane(cur.info, ws * C::SUBS + sb);
+      flags |= inf;
+      none &= inf;
+    }
+    if (!any_live || none) return;
+    // S^T: lane = row, register 4 j + i of tile kt = key 32 kt + 8 j + 4 h + i
+    f32x16 s[C::NS];
+#pragma unroll
+    for (int kt = 0; kt < C::NS; ++kt) {
+#pragma unroll
+      for (int r = 0; r < 16; ++r) s[kt][r] = 0.0f;
+#pragma unroll
+      for (int i = 0; i < C::NQ; ++i) {
+        const qvec kf = *reinterpret_cast<const qvec *>(kb + kat[i] + 32 * kt * C::ROW);
+        if constexpr (sizeof(T) == 2) {
+          s[kt] = mfma_bf16(kf, qf[i], s[kt]);
+        } else {
+#pragma unroll
+          for (int e = 0; e < 4; ++e) s[kt] = mfma_f32(kf[e], qf[i][e], s[kt]);
+        }
+      }
+    }
+    bool move = !all_set;
+    uint32_t hidden = 0;                 // careful run: registers of S not to be seen
+    const bool mask = (flags & (kMask | kNone)) != 0;
+    if (mask) {
+      masked = move = true;
+#pragma unroll
+      for (int sb = 0; sb < C::SUBS; ++sb) {
+        const int idx = ws * C::SUBS + sb;
+        const int place = __builtin_amdgcn_readlane(cur.place, idx);
+        const int valid = __builtin_amdgcn_readlane(cur.info, idx) >> 8 & 31;  // 0 beyond the end
+        const int ei = place & 4095, slot = (place >> 12) * 16;
+        const Entry en = entry(ei);
+        int lim = 0;
+        if (en.own & seq_bit) lim = qslot + 1 - slot;
+        else if (en.below & seq_bit) lim = 16;
+        lim = live ? min(lim, valid) : valid;
+#pragma unroll
+        for (int j = 0; j < 2; ++j)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const bool hide = 8 * j + 4 * h + i >= lim;
+            float &z = reinterpret_cast<float *>(&s[sb / 2])[8 * (sb & 1) + 4 * j + i];
+            z = hide ? -INFINITY : z;
+            if constexpr (CAREFUL) hidden |= hide ? 1u << (8 * sb + 4 * j + i) : 0u;
+          }
+      }
+    }
+    // P as the B operand of O^T += V^T P^T: registers 8 ks .. 8 ks + 7 of a step's 16
+    // keys ks, rounded to V's type
+    pvec p[C::KEYS / C::PK];
+    float sum;
+    auto terms = [&](float r) __attribute__((always_inline)) {
+      float part[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+      for (int kt = 0; kt < C::NS; ++kt)
+#pragma unroll
+        for (int x = 0; x < 16; ++x) {
+          const float e = __builtin_amdgcn_exp2f(__builtin_fmaf(s[kt][x], a.sl2, -r));
+          part[x & 3] += e;
+          if constexpr (sizeof(T) == 2) p[2 * kt + x / 8][x % 8] = (__bf16)e;
+          else p[x] = e;
+        }
+      sum = (part[0] + part[1]) + (part[2] + part[3]);
+    };
+    if (!move) {
+      terms(ref);
+      move = ballot(!(sum < kMoveAt)) != 0;
+    }
+    if (move) {
+      float mx = -INFINITY;
+#pragma unroll
+      for (int kt = 0; kt < C::NS; ++kt)
+#pragma unroll
+        for (int x = 0; x < 16; ++x) mx = fmaxf(mx, s[kt][x]);
+      const float to = fmaxf(ref, swap_halves_max(mx) * a.sl2);
+      if (ballot(to > ref)) {
+        const float by = to == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(ref - to);
+        l *= by;
+#pragma unroll
+        for (int d = 0; d < C::DT; ++d)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) o[d][r] *= by;
+        ref = to;
+      }
+      terms(ref == -INFINITY ? 0.0f : ref);
+      if (!mask) all_set = true;
+    }
+    l += sum;
+    if (!CAREFUL || !mask) {
+      if constexpr (sizeof(T) == 2) {
+        // keys 16 ks + 4 h + i and 16 ks + 8 + 4 h + i: the order that P has
+#pragma unroll
+        for (int ks = 0; ks < C::KEYS / 16; ++ks)
+#pragma unroll
+          for (int d = 0; d < C::DT; ++d)
+            o[d] = mfma_bf16(read_transposed(vb + vat[d] + 16 * ks * C::ROW, 8 * C::ROW), p[ks],
+                             o[d]);
+      } else {
+#pragma unroll
+        for (int x = 0; x < 16; ++x)
+#pragma unroll
+          for (int d = 0; d < C::DT; ++d)
+            o[d] = mfma_f32(*reinterpret_cast<const float *>(
+                                vb + vat[d] + (8 * (x / 4) + x % 4) * C::ROW),
+                            p[x], o[d]);
+      }
+    } else if constexpr (CAREFUL) {
+      // 16 keys of P at a time go through the buffer that a careful run does not load
+      // into; a hidden key is marked by -1
+      float *scr = reinterpret_cast<float *>(lds + C::BUF) + wave * 512;
+      const float r = ref == -INFINITY ? 0.0f : ref;
+#pragma unroll
+      for (int ks = 0; ks < C::KEYS / 16; ++ks) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const float z = reinterpret_cast<const float *>(&s[ks / 2])[8 * (ks & 1) + e];
+          scr[(8 * (e / 4) + 4 * h + e % 4) * 32 + lr] =
+              hidden >> (8 * ks + e) & 1
+                  ? -1.0f : __builtin_amdgcn_exp2f(__builtin_fmaf(z, a.sl2, -r));
+        }
+        __builtin_amdgcn_s_waitcnt(0);
+        __builtin_amdgcn_wave_barrier();
+        for (int key = 0; key < 16; ++key) {
+          const float pk = scr[key * 32 + lr];
+          const char *vr = vb + (16 * ks + key) * C::ROW;
+#pragma unroll
+          for (int d = 0; d < C::DT; ++d)
+#pragma unroll
+            for (int x = 0; x < 16; ++x) {
+              const int c = 32 * d + 8 * (x / 4) + 4 * h + x % 4;
+              const float vv = (float)*reinterpret_cast<const T *>(
+                  vr + v_piece<T, D>(key, c * C::ES / 16) * 16 + c * C::ES % 16);
+              if (!(pk < 0.0f)) o[d][x] += pk * vv;
+            }
+        }
+        __builtin_amdgcn_wave_barrier();
+      }
+    }
+  };
+  auto clear = [&]() __attribute__((always_inline)) {
 #pragma unroll
     for (int d = 0; d < C::DT; ++d)
 #pragma unroll
       for (int r = 0; r < 16; ++r) o[d][r] = 0.0f;
     ref = -INFINITY;
     l = 0.0f;
-    bool all_set = false, masked = false;
+    all_set = masked = false;
+  };
+  // a step's loads have landed, and every wave is done with the other buffer
+  auto arrive = [&]() __attribute__((always_inline)) {
+    __builtin_amdgcn_s_waitcnt(0);
+    __syncthreads();
+  };
+
+  clear();
+  {
     Window win = fill(0), nxt = win;
-    if (steps > 0) issue(win, 0, 0);
-    for (int st = 0; st < steps; ++st) {
+    issue(win, 0, 0);
+    for (int st = 0; st < steps; st += 2) {
       const int ws = st % WSTEPS;
-      const int buf = careful ? 0 : st & 1;
       if (ws == 0 && st + WSTEPS < steps) nxt = fill((st + WSTEPS) * C::SUBS);
-      // this step's loads have landed, and every wave is done with the other buffer
-      __builtin_amdgcn_s_waitcnt(0);
-      __syncthreads();
-      const Window cur = win;
-      if (ws == WSTEPS - 1) win = nxt;
-      if (!careful && st + 1 < steps) issue(win, (st + 1) % WSTEPS, buf ^ 1);
-      int flags = 0, none = kNone;
-#pragma unroll
-      for (int sb = 0; sb < C::SUBS; ++sb) {
-        const int inf = __builtin_amdgcn_readlane(cur.info, ws * C::SUBS + sb);
-        flags |= inf;
-        none &= inf;
+      arrive();
+      if (st + 1 < steps) issue(win, ws + 1, 1);
+      step(win, ws, std::integral_constant<int, 0>{}, std::false_type{});
+      if (st + 1 < steps) {
+        arrive();
+        if (st + 2 < steps) issue(ws + 2 < WSTEPS ? win : nxt, (ws + 2) % WSTEPS, 0);
+        step(win, ws + 1, std::integral_constant<int, 1>{}, std::false_type{});
       }
-      if (any_live && !none) {
-        // S^T: lane = row, register 4 j + i of tile kt = key 32 kt + 8 j + 4 h + i
-        const char *kb = lds + buf * C::BUF;
-        f32x16 s[C::NS];
-#pragma unroll
-        for (int kt = 0; kt < C::NS; ++kt) {
-#pragma unroll
-          for (int r = 0; r < 16; ++r) s[kt][r] = 0.0f;
-          const int key = 32 * kt + lr;
-#pragma unroll
-          for (int i = 0; i < C::NQ; ++i) {
-            const qvec kf = *reinterpret_cast<const qvec *>(
-                kb + key * C::ROW + k_piece<T, D>(key, 2 * i + h) * 16);
-            if constexpr (sizeof(T) == 2) {
-              s[kt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[i], s[kt], 0, 0, 0);
-            } else {
-#pragma unroll
-              for (int e = 0; e < 4; ++e)
-                s[kt] = __builtin_amdgcn_mfma_f32_32x32x2f32(kf[e], qf[i][e], s[kt], 0, 0, 0);
-            }
-          }
-        }
-        bool move = !all_set;
-        uint32_t hidden = 0;                 // careful run: registers of S not to be seen
-        const bool mask = (flags & (kMask | kNone)) != 0;
-        if (mask) {
-          masked = move = true;
-#pragma unroll
-          for (int sb = 0; sb < C::SUBS; ++sb) {
-            const int idx = ws * C::SUBS + sb;
-            const int inf = __builtin_amdgcn_readlane(cur.info, idx);
-            const int ei = __builtin_amdgcn_readlane(cur.ent, idx);
-            const int slot = __builtin_amdgcn_readlane(cur.slot, idx);
-            const int valid = (inf >> 8) & 31;          // 0 beyond the unit's end
-            const Entry *en = ents_lds ? &sh_ent[ei] : &ents[ei];
-            int lim = 0;
-            if (en->own & seq_bit) lim = qslot + 1 - slot;
-            else if (en->below & seq_bit) lim = 16;
-            lim = live ? min(lim, valid) : valid;
-#pragma unroll
-            for (int j = 0; j < 2; ++j)
-#pragma unroll
-              for (int i = 0; i < 4; ++i)
-                if (8 * j + 4 * h + i >= lim) {
-                  s[sb / 2][8 * (sb & 1) + 4 * j + i] = -INFINITY;
-                  if (careful) hidden |= 1u << (8 * sb + 4 * j + i);
-                }
-          }
-        }
-        float p[C::NS][16], sum;
-        auto terms = [&](float r) __attribute__((always_inline)) {
-          float part[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-          for (int kt = 0; kt < C::NS; ++kt)
-#pragma unroll
-            for (int x = 0; x < 16; ++x) {
-              p[kt][x] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[kt][x], a.sl2, -r));
-              part[x & 3] += p[kt][x];
-            }
-          sum = (part[0] + part[1]) + (part[2] + part[3]);
-        };
-        if (!move) {
-          terms(ref);
-          move = ballot(!(sum < kMoveAt)) != 0;
-        }
-        if (move) {
-          float mx = -INFINITY;
-#pragma unroll
-          for (int kt = 0; kt < C::NS; ++kt)
-#pragma unroll
-            for (int x = 0; x < 16; ++x) mx = fmaxf(mx, s[kt][x]);
-          mx = swap_halves_max(mx) * a.sl2;
-          const float to = fmaxf(ref, mx);
-          const float by = to == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(ref - to);
-          l *= by;
-#pragma unroll
-          for (int d = 0; d < C::DT; ++d)
-#pragma unroll
-            for (int r = 0; r < 16; ++r) o[d][r] *= by;
-          ref = to;
-          terms(to == -INFINITY ? 0.0f : to);
-          if (!mask) all_set = true;
-        }
-        l += sum;
-        // O^T += V^T P^T
-        const char *vb = lds + 2 * C::BUF + buf * C::BUF;
-        if (!careful) {
-          if constexpr (sizeof(T) == 2) {
-            // two transposing reads give the lane's column 32 d + lr of the keys
-            // 16 ks + 4 h + i and 16 ks + 8 + 4 h + i, the order that P has: lane x of
-            // 16 addresses four columns from 4 (x % 4) of key x / 4
-            const int x16 = lane & 15, col = ((lane >> 4) & 1) * 16 + 4 * (x16 & 3);
-#pragma unroll
-            for (int ks = 0; ks < C::KEYS / 16; ++ks) {
-              bf16x8 pf;
-#pragma unroll
-              for (int e = 0; e < 8; ++e) pf[e] = (__bf16)p[ks / 2][8 * (ks & 1) + e];
-#pragma unroll
-              for (int d = 0; d < C::DT; ++d) {
-                bf16x4 v2[2];
-#pragma unroll
-                for (int y = 0; y < 2; ++y) {
-                  const int key = 16 * ks + 8 * y + 4 * h + (x16 >> 2);
-                  const int c = 32 * d + col;
-                  typedef short s16x4 __attribute__((ext_vector_type(4)));
-                  typedef __attribute__((address_space(3))) s16x4 *P4;
-                  const s16x4 tv = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-                      (P4)(vb + key * C::ROW + v_piece<T, D>(key & 15, c / 8) * 16 + c % 8 * 2));
-                  v2[y] = __builtin_bit_cast(bf16x4, tv);
-                }
-                const bf16x8 vf = __builtin_shufflevector(v2[0], v2[1], 0, 1, 2, 3, 4, 5, 6, 7);
-                o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, pf, o[d], 0, 0, 0);
-              }
-            }
-          } else {
-#pragma unroll
-            for (int x = 0; x < 16; ++x) {
-              const int key = 8 * (x / 4) + 4 * h + x % 4;
-#pragma unroll
-              for (int d = 0; d < C::DT; ++d) {
-                const int c = 32 * d + lr;
-                const float vf = *reinterpret_cast<const float *>(
-                    vb + key * C::ROW + v_piece<T, D>(key & 15, c / 4) * 16 + c % 4 * 4);
-                o[d] = __builtin_amdgcn_mfma_f32_32x32x2f32(vf, p[0][x], o[d], 0, 0, 0);
-              }
-            }
-          }
-        } else {
-          // A key that a row may not see has p = 0, but 0 times an infinite or NaN
-          // value is not 0: here it is left out (marked by -1).  16 keys of P at a time
-          // go through the buffer that a careful run does not load into.
-          float *scr = reinterpret_cast<float *>(lds + C::BUF) + wave * 512;
-#pragma unroll
-          for (int ks = 0; ks < C::KEYS / 16; ++ks) {
-#pragma unroll
-            for (int e = 0; e < 8; ++e)
-              scr[(8 * (e / 4) + 4 * h + e % 4) * 32 + lr] =
-                  hidden >> (8 * ks + e) & 1 ? -1.0f : p[ks / 2][8 * (ks & 1) + e];
-            __builtin_amdgcn_s_waitcnt(0);
-            __builtin_amdgcn_wave_barrier();
-            for (int key = 0; key < 16; ++key) {
-              const float pk = scr[key * 32 + lr];
-              const char *vr = vb + (16 * ks + key) * C::ROW;
-#pragma unroll
-              for (int d = 0; d < C::DT; ++d)
-#pragma unroll
-                for (int r = 0; r < 16; ++r) {
-                  const int c = 32 * d + 8 * (r / 4) + 4 * h + r % 4;
-                  const float vv = (float)*reinterpret_cast<const T *>(
-                      vr + v_piece<T, D>(key, c * C::ES / 16) * 16 + c * C::ES % 16);
-                  if (!(pk < 0.0f)) o[d][r] += pk * vv;
-                }
-            }
-            __builtin_amdgcn_wave_barrier();
-          }
-        }
-      }
-      if (careful && st + 1 < steps) {
-        __syncthreads();                       // every wave is done with the one buffer
-        issue(win, (st + 1) % WSTEPS, 0);
-      }
+      if (ws + 2 == WSTEPS) win = nxt;
     }
-    if (careful) break;
-    bool finite = true;
+  }
+  // A key that a row may not see has p = 0, but 0 times an infinite or NaN value is not
+  // 0.  So a unit that hid keys and whose outputs are not all finite runs once more, its
+  // steps with hidden keys summed key by key, without them.
+  bool finite = true;
 #pragma unroll
-    for (int d = 0; d < C::DT; ++d)
+  for (int d = 0; d < C::DT; ++d)
 #pragma unroll
-      for (int r = 0; r < 16; ++r) finite = finite && __builtin_isfinite(o[d][r]);
-    if (!__syncthreads_or(live && masked && !finite)) break;
-    careful = true;
+    for (int r = 0; r < 16; ++r) finite = finite && __builtin_isfinite(o[d][r]);
+  if (__syncthreads_or(live && masked && !finite)) {
+    clear();
+    for (int st = 0; st < steps; ++st) {
+      const Window win = fill(st / WSTEPS * kWave);
+      issue(win, st % WSTEPS, 0);
+      arrive();
+      step(win, st % WSTEPS, std::integral_constant<int, 0>{}, std::true_type{});
+      __syncthreads();                         // every wave is done with the buffer
+    }
   }
   if (ballot(stale)) {
     if (lane == 0) status_error(a.status, ARBOR_EINVAL);

@@ -151,11 +151,65 @@ def test_tiles_never_exceed_their_bound():
 
 def test_the_binding_checks_shapes_types_and_places():
     cpu = torch.zeros(3, dtype=torch.int32)
-    for f in (lambda: L._is(cpu, "x", torch.int64, 3), lambda: L._is(cpu, "x", torch.int32, 4),
-              lambda: L._is(cpu, "x", torch.int32, 3), lambda: L._packed(cpu, cpu),
-              lambda: L._rows(torch.zeros(2, 8), "q", torch.bfloat16, 2, 8),
-              lambda: L._rows(torch.zeros(2, 8), "q", torch.float32, 3, 8),
-              lambda: L._rows(torch.zeros(2, 8), "q", torch.float32, 2, 9),
-              lambda: L._rows(torch.zeros(2, 8), "q", torch.float32, 2, 8)):
+    rows = torch.zeros(2, 8)
+    for f in (lambda: L._is(cpu, "x", torch.int64, (3,), -1),
+              lambda: L._is(cpu, "x", torch.int32, (4,), -1),
+              lambda: L._is(cpu, "x", torch.int32, (3,), -1),
+              lambda: L._is(cpu, "x", torch.int32, (3,), 0),
+              lambda: L._packed(cpu, cpu, 0), lambda: L._bytes(cpu, "x", 0),
+              lambda: L._rows(rows, "q", torch.bfloat16, 2, 8, -1),
+              lambda: L._rows(rows, "q", torch.float32, 3, 8, -1),
+              lambda: L._rows(rows, "q", torch.float32, 2, 9, -1),
+              lambda: L._rows(rows, "q", torch.float32, 2, 8, 0),
+              lambda: L._record(rows, "r", torch.float32, (2, 9)),
+              lambda: L._record(rows, "r", torch.float32, (2, 8))):
         with pytest.raises(ValueError):
             f()
+
+
+def test_descriptors_follow_the_state(monkeypatch):
+    """What a KVState's tensors are is read again when a field is set or a tensor is moved."""
+    monkeypatch.setattr(L, "_dev", lambda t, name: None if t is None else t.data_ptr())
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: -1)     # CPU tensors here
+    z = lambda n: torch.zeros(n, dtype=torch.int32)  # noqa: E731
+    kv = L.KVState(z(4), z(4), z(5), z(5), z(4), z(9), torch.zeros(1, 9, 2, 16, 64),
+                   torch.zeros(1, 9, 2, 16, 64), z(9), z(9), z(1), 1, 2, 4, 64, 16, L.F32, 100)
+    tree = lambda: L._descriptors(kv)[2]._obj  # noqa: E731
+    geom = lambda: L._descriptors(kv)[1]._obj  # noqa: E731
+    assert L._descriptors(kv) == L._descriptors(kv) and tree() is tree()
+    assert tree().num_nodes == 4 and L._descriptors(kv)[4] == kv.n_full.data_ptr()
+    buf = z(20)
+    kv.parent = buf[:4]
+    assert tree().parent == buf.data_ptr() and tree().num_nodes == 4
+    kv.parent = buf[:7]                                  # the same memory, more blocks
+    assert tree().num_nodes == 7
+    kv.q_per_kv, kv.num_tokens = 8, 300
+    assert geom().q_per_kv == 8 and tree().num_tokens == 300
+    kv.n_kept.data = z(64)
+    assert tree().n_kept == kv.n_kept.data_ptr()
+    copy = kv.clone()
+    assert L._descriptors(copy)[2]._obj.parent == copy.parent.data_ptr() != tree().parent
+    kv.k.resize_(1, 5, 2, 16, 64)
+    assert geom().num_pages == 5
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
+    with pytest.raises(ValueError):
+        L._descriptors(kv)
+
+
+def test_append_struct_layout(tmp_path):
+    """The binding's arbor_append_t has the C compiler's size and offsets."""
+    import os
+    import subprocess
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    names = [f[0] for f in L.Append._fields_]
+    src = tmp_path / "layout.c"
+    src.write_text("#include <stdio.h>\n#include <stddef.h>\n#include \"arbor.h\"\nint main(void) {"
+                   'printf("%zu\\n", sizeof(arbor_append_t));' +
+                   "".join(f'printf("%zu\\n", offsetof(arbor_append_t, {n}));' for n in names) +
+                   "return 0; }\n")
+    exe = tmp_path / "layout"
+    subprocess.run(["gcc", "-D__HIP_PLATFORM_AMD__", "-I", os.path.join(root, "include"), "-I",
+                    "/opt/rocm/include", str(src), "-o", str(exe)], check=True)
+    got = [int(x) for x in subprocess.run([str(exe)], check=True, capture_output=True,
+                                          text=True).stdout.split()]
+    assert got == [ctypes.sizeof(L.Append)] + [getattr(L.Append, n).offset for n in names]
