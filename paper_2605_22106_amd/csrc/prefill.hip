@@ -42,12 +42,16 @@ constexpr float kLn2 = 0.6931471805599453f;
 // until then p = 2^(s - ref) may exceed 1, which costs no precision in fp32 or bf16
 // and leaves V 2^100 of headroom, and a step needs neither a max nor a rescale.
 constexpr float kMoveAt = 65536.0f;
-// Workgroups that the chip holds at a time (two to each of 256 CUs).  Parts for 384 or 768
-// of them instead: 16 ragged blocks over a thinned tree, four layers, 158 and 197 us
-// against 149; 64 drafts below 32,000 tokens, two layers, 285 and 266 against 231.  The
-// shortest part at 32, 16 and 8 sub-pages: 163, 163 and 149 us, and 239, 231 and 230.
+// Workgroups that the chip holds at a time (two to each of 256 CUs).  Parts for 256 of them
+// instead: 64 drafts below 32,000 tokens, two layers, 277 us against 220; 16 ragged blocks
+// over a tree, four layers, 240 against 206.
 constexpr int kSlots = 512;
-constexpr int kMinPart = 4;             // sub-pages of the shortest part
+// Sub-pages of a step, and steps of the shortest part: a part's fixed work (its way to its
+// first key, its sums to memory and back) is worth about two steps.  At 2, 4 and 8 steps
+// of 64 keys the 16 blocks above take 206, 206 and 222 us, 16 over a thinned tree 139, 149
+// and 149; at one and two steps of 32 keys 48 fp32 tokens over 160 take 26 us, at four 32.
+__host__ __device__ constexpr int step_subs(int bytes) { return bytes == 2 ? 4 : 2; }
+constexpr int kMinSteps = 2;
 
 struct Header {
   int64_t magic;
@@ -59,8 +63,6 @@ struct Tile {
   int32_t e0, ne;       // sequences that they belong to
   int32_t n_ent;        // chain blocks, at entry kMaxSeq... (see entry_base)
   int32_t n_sub;        // sub-pages of all of them
-  int32_t parts;        // 1: written directly
-  int32_t part0;        // first partial
 };
 
 // One chain block of a tile, root first.
@@ -86,7 +88,7 @@ struct PlanPtrs {
   Tile *tiles;
   Entry *ents;
   Unit *units;
-  int32_t *split;       // tiles in parts
+  int4 *split;          // tiles in parts: t0, nt, first partial, parts
   int2 *tok;            // per packed token: own slot, sequence within its tile
   int64_t tiles_cap, units_cap;
 };
@@ -99,7 +101,7 @@ inline int64_t tile_bound(int G, int n_seq, int64_t n_tokens) {
   const int64_t b = 2 * (n_tokens / tokens_per_tile(G)) + n_seq / kMaxSeq + 2;
   return b < n_tokens ? b : n_tokens;
 }
-inline int target_parts(int Hkv) {
+__host__ __device__ inline int target_parts(int Hkv) {
   const int t = kSlots / Hkv;
   return t > 0 ? t : 1;
 }
@@ -114,7 +116,7 @@ PlanPtrs carve_plan(const arbor_geom_t *g, int n_seq, int n_tokens, void *plan, 
   p.tiles = cv.take<Tile>(p.tiles_cap + 1);
   p.ents = cv.take<Entry>((size_t)kMaxSeq * ((size_t)n_seq + p.tiles_cap + 1));
   p.units = cv.take<Unit>(p.units_cap);
-  p.split = cv.take<int32_t>(target_parts(g->num_kv_heads) + 1);
+  p.split = cv.take<int4>(target_parts(g->num_kv_heads) + 1);
   p.tok = cv.take<int2>((size_t)n_tokens + 1);
   if (need) *need = cv.off;
   if (!cv.ok) p.head = nullptr;
@@ -129,28 +131,30 @@ __host__ __device__ inline int64_t entry_base(int tile, int e0) {
 }
 
 // ---- plan ---------------------------------------------------------------------
-// Cuts the packed tokens into tiles.  A tile takes the next block's tokens when all
-// of them fit (two blocks in one tile read the blocks that they share once, and
-// nothing twice); a block of more tokens than a tile holds starts its own.  One
-// wave goes from tile to tile, 64 blocks at a time in its lanes.
-__global__ __launch_bounds__(1024) void plan_tiles(Tree t, int G, int Hkv, int P,
-                                                   const int32_t *__restrict__ nodes, int n_seq,
-                                                   const int32_t *__restrict__ cu, int n_tokens,
-                                                   PlanPtrs p, int32_t *status) {
-  if (threadIdx.x == 0) p.head->magic = 0;
-  if (status_failed(status)) return;
-  int err = 0;
-  if (threadIdx.x == 0 && (cu[0] != 0 || cu[n_seq] < 0 || cu[n_seq] > n_tokens)) err = 1;
+// Whether the request is sound: ids, cu, and as many resident tokens as are new.  Called
+// by a whole workgroup.
+// cu_lds, if given, holds cu afterwards.
+__device__ bool request_ok(const Tree &t, const int32_t *__restrict__ nodes, int n_seq,
+                           const int32_t *__restrict__ cu, int n_tokens, int32_t *cu_lds) {
+  int err = threadIdx.x == 0 && (cu[0] != 0 || cu[n_seq] < 0 || cu[n_seq] > n_tokens);
   for (int e = threadIdx.x; e < n_seq; e += blockDim.x) {
-    const int i = nodes[e], m = cu[e + 1] - cu[e];
+    const int i = nodes[e], c0 = cu[e], c1 = cu[e + 1], m = c1 - c0;
+    if (cu_lds) {
+      cu_lds[e] = c0;
+      if (e == n_seq - 1) cu_lds[n_seq] = c1;
+    }
     if (i < 0 || i >= t.V || m < 0 || m > n_tokens) err = 1;
     else if (m > t.n_kept[i]) err = 1;
   }
-  if (__syncthreads_or(err)) {
-    if (threadIdx.x == 0) status_error(status, ARBOR_EINVAL);
-    return;
-  }
-  if (threadIdx.x >= kWave) return;
+  return !__syncthreads_or(err);
+}
+
+// Cuts the packed tokens into tiles; one wave.  A tile takes the next block's tokens when
+// all of them fit (two blocks in one tile read the blocks that they share once, and
+// nothing twice); a block of more tokens than a tile holds starts its own.  The wave goes
+// from tile to tile, 64 blocks at a time in its lanes.  Returns how many tiles there are.
+__device__ int cut_tiles(int G, int n_seq, const int32_t *cu, Tile *tiles, int tiles_cap,
+                         int32_t *status) {
   const int lane = lane_id(), TQ = tokens_per_tile(G);
   int e = 0, off = 0, k = 0;               // off: tokens of sequence e already in tiles
   while (e < n_seq) {
@@ -167,7 +171,7 @@ __global__ __launch_bounds__(1024) void plan_tiles(Tree t, int G, int Hkv, int P
     if (first > TQ) {
       const int full = first / TQ;
       for (int x = lane; x < full; x += kWave)
-        if (k + x < p.tiles_cap) p.tiles[k + x] = Tile{t0 + x * TQ, TQ, e, 1, 0, 0, 1, 0};
+        if (k + x < tiles_cap) tiles[k + x] = Tile{t0 + x * TQ, TQ, e, 1, 0, 0};
       k += full;
       off += full * TQ;
       if (full * TQ == first) {
@@ -179,99 +183,100 @@ __global__ __launch_bounds__(1024) void plan_tiles(Tree t, int G, int Hkv, int P
     const int sum = wave_inclusive_scan(min(m, TQ + 1));
     const int fit = popc(ballot(sum <= TQ));          // sums ascend
     const int nt = lane_value(sum, fit - 1);
-    if (lane == 0 && k < p.tiles_cap) p.tiles[k] = Tile{t0, nt, e, fit, 0, 0, 1, 0};
+    if (lane == 0 && k < tiles_cap) tiles[k] = Tile{t0, nt, e, fit, 0, 0};
     ++k;
     e += fit;
     off = 0;
   }
-  if (lane == 0) {
-    if (k > p.tiles_cap) status_error(status, ARBOR_ECORRUPT);   // (the bound holds)
-    p.head->n_seq = n_seq;
-    p.head->n_tokens = n_tokens;
-    p.head->V = t.V;
-    p.head->G = G;
-    p.head->Hkv = Hkv;
-    p.head->page_size = P;
-    p.head->n_tiles = k;
+  if (k > tiles_cap) {                                // (the bound holds)
+    if (lane == 0) status_error(status, ARBOR_ECORRUPT);
+    k = tiles_cap;
   }
+  return k;
 }
 
-// One wave per tile: the chains of its sequences, merged by ascending id.
-__global__ __launch_bounds__(64) void plan_chains(Tree t, const int32_t *__restrict__ nodes,
-                                                  const int32_t *__restrict__ cu, PlanPtrs p,
-                                                  int32_t *status) {
-  __shared__ int32_t chain[MAXD][kWave + 1];     // leaf first
-  if (status_failed(status) || (int)blockIdx.x >= p.head->n_tiles) return;
+__device__ void write_header(const PlanPtrs &p, int V, int G, int Hkv, int P, int n_seq,
+                             int n_tokens, int n_tiles) {
+  p.head->n_seq = n_seq;
+  p.head->n_tokens = n_tokens;
+  p.head->V = V;
+  p.head->G = G;
+  p.head->Hkv = Hkv;
+  p.head->page_size = P;
+  p.head->n_tiles = n_tiles;
+}
+
+constexpr int kCol = kWave + 1;          // chains lie side by side, [MAXD][kCol], leaf first
+
+// The chain of the block x (none for x < 0) into column col: its length, or an error code.
+__device__ int walk_chain(const int32_t *parent, int x, int32_t *chain, int col) {
+  int depth = 0;
+  while (x >= 0) {
+    if (depth == MAXD) return ARBOR_EUNSUPPORTED;
+    chain[depth * kCol + col] = x;
+    ++depth;
+    const int up = parent[x];
+    if (up >= x) return ARBOR_EINVAL;
+    x = up;
+  }
+  return depth;
+}
+
+// Tile k's chain blocks, and its tokens' own slots; one wave.  Lane j's sequence has its
+// chain, `depth` blocks, in column col.  Blocks come in ascending order of ids, so the next
+// one is the smallest id that any lane has next; 64 of them wait in the lanes.
+__device__ void merge_chains(const Tree &t, const int32_t *cu, const PlanPtrs &p, int k,
+                             Tile *tile, const int32_t *chain, int col, int depth) {
   const int lane = lane_id();
-  Tile tl = p.tiles[blockIdx.x];
-  Entry *ents = p.ents + entry_base(blockIdx.x, tl.e0);
-  const int e = tl.e0 + lane;
-  int lo = 0, hi = 0, x = -1, newest = -1;
+  const Tile tl = *tile;
+  Entry *ents = p.ents + entry_base(k, tl.e0);
+  int lo = 0, hi = 0, leaf = -1, newest = -1;
   if (lane < tl.ne) {
-    const int c0 = cu[e], c1 = cu[e + 1];
+    const int c0 = cu[tl.e0 + lane], c1 = cu[tl.e0 + lane + 1];
     lo = max(c0, tl.t0);
     hi = min(c1, tl.t0 + tl.nt);
     if (hi > lo) {
-      x = nodes[e];
-      newest = t.n_kept[x] - (c1 - hi) - 1;       // slot of the sequence's last token here
+      leaf = chain[col];
+      newest = t.n_kept[leaf] - (c1 - hi) - 1;    // slot of the sequence's last token here
     }
   }
-  const int leaf = x;
-  int depth = 0;
-  bool bad = false, deep = false;
-  for (int y = x; ballot(y >= 0);) {
-    if (y >= 0) {
-      chain[depth][lane] = y;
-      ++depth;
-      const int up = t.parent[y];
-      if (up >= y) bad = true;
-      else if (up >= 0 && depth == MAXD) deep = true;
-      y = bad || deep ? -1 : up;
+  int subs = 0, n = 0;
+  Entry mine{};
+  auto flush = [&](int cnt) {
+    int need = 0;
+    if (lane < cnt) {
+      if (mine.below != mine.own) mine.limit = t.n_kept[mine.node];
+      mine.po = (int32_t)t.page_off[mine.node];
+      need = (mine.limit + 15) / 16;
     }
-  }
-  if (ballot(bad || deep)) {
-    if (lane == 0) status_error(status, ballot(bad) ? ARBOR_EINVAL : ARBOR_EUNSUPPORTED);
-    return;
-  }
-  // the smallest id among the lanes' next blocks, until none is left
-  int at = depth - 1, n = 0;
+    const int inc = wave_inclusive_scan(need);
+    mine.sub0 = subs + inc - need;
+    if (lane < cnt) ents[(n - 1) / kWave * kWave + lane] = mine;
+    subs += lane_value(inc, kWave - 1);
+  };
+  int at = leaf >= 0 ? depth - 1 : -1;
   while (true) {
-    const int next = at >= 0 ? chain[at][lane] : INT32_MAX;
+    const int next = at >= 0 ? chain[at * kCol + col] : INT32_MAX;
     const int mn = wave_allreduce(next, [](int a, int b) { return a < b ? a : b; });
     if (mn == INT32_MAX) break;
     const bool here = next == mn;
     const uint64_t below = ballot(here), own = ballot(here && mn == leaf);
-    const int last = wave_allreduce(here && mn == leaf ? newest : -1,
-                                    [](int a, int b) { return a > b ? a : b; });
-    if (lane == 0) {
-      ents[n].node = mn;
-      ents[n].limit = last + 1;
-      ents[n].below = below;
-      ents[n].own = own;
+    int last = -1;
+    if (own) last = wave_allreduce(here && mn == leaf ? newest : -1,
+                                   [](int a, int b) { return a > b ? a : b; });
+    if (lane == n % kWave) {
+      mine.node = mn;
+      mine.limit = last + 1;
+      mine.below = below;
+      mine.own = own;
     }
     at -= here ? 1 : 0;
-    ++n;
+    if (++n % kWave == 0) flush(kWave);
   }
-  __threadfence_block();
-  __builtin_amdgcn_wave_barrier();
-  int subs = 0;
-  for (int b = 0; b < n; b += kWave) {
-    const int y = b + lane;
-    int mine = 0;
-    if (y < n) {
-      const int node = ents[y].node;
-      const int limit = ents[y].below == ents[y].own ? ents[y].limit : t.n_kept[node];
-      ents[y].limit = limit;
-      ents[y].po = (int32_t)t.page_off[node];
-      mine = (limit + 15) / 16;
-    }
-    const int inc = wave_inclusive_scan(mine);
-    if (y < n) ents[y].sub0 = subs + inc - mine;
-    subs += lane_value(inc, kWave - 1);
-  }
+  if (n % kWave) flush(n % kWave);
   if (lane == 0) {
-    p.tiles[blockIdx.x].n_ent = n;
-    p.tiles[blockIdx.x].n_sub = subs;
+    tile->n_ent = n;
+    tile->n_sub = subs;
   }
   // own slot and sequence of each of its tokens
   for (int j = 0; j < tl.ne; ++j) {
@@ -280,87 +285,169 @@ __global__ __launch_bounds__(64) void plan_chains(Tree t, const int32_t *__restr
   }
 }
 
-// Parts of the tiles, longest first.
-__global__ __launch_bounds__(1024) void plan_units(PlanPtrs p, int target, int32_t *status) {
+// Cuts long tiles into parts and lists all parts, longest first; a workgroup of up to 16
+// waves.  Parts are in proportion to a tile's keys, rounded down: all parts together are no
+// more than `target` and the uncut tiles, so that they run at once.
+__device__ void list_units(const PlanPtrs &p, const Tile *tiles, int n, int target, int min_part,
+                           int32_t *status) {
   constexpr int NB = 256;
-  __shared__ int64_t sm[17];
+  __shared__ int64_t sm[2 * 16];
   __shared__ int32_t bucket[NB + 1], longest;
-  if (status_failed(status)) return;
-  const int n = p.head->n_tiles, nt = blockDim.x, tid = threadIdx.x;
-  const int per = (n + nt - 1) / nt;
-  const int r0 = min(n, tid * per), r1 = min(n, r0 + per);
+  const int nt = blockDim.x, tid = threadIdx.x, lane = lane_id();
+  const Tile none{};
+  const Tile first = tid < n ? tiles[tid] : none;
   int64_t subs = 0;
-  for (int k = r0; k < r1; ++k) subs += p.tiles[k].n_sub;
+  for (int k = tid; k < n; k += nt) subs += k == tid ? first.n_sub : tiles[k].n_sub;
   const int64_t total = block_sum(subs, sm);
   for (int b = tid; b <= NB; b += nt) bucket[b] = 0;
   if (tid == 0) longest = 1;
   __syncthreads();
-  // Parts in proportion, rounded down: all parts together are no more than `target` and the
-  // uncut tiles, so that they run at once (rounded up they were 576 for 512 places, two
-  // rounds: 64 drafts below 32,000 tokens 131 us, now 92)
-  int64_t parts = 0, cut = 0;
+  const double per = total > 0 ? (double)target / (double)total : 0.0;
+  auto share = [&](int s) { return max(1, min((int)(s * per), s / min_part)); };
+  auto length = [](int s, int np) { return (s + np - 1) / np; };
+  int64_t v[2] = {0, 0}, ex[2], tot[2];        // parts of cut tiles, cut tiles
   int far = 0;
-  for (int k = r0; k < r1; ++k) {
-    const int s = p.tiles[k].n_sub;
-    const int64_t share = total > 0 ? (int64_t)s * target / total : 1;
-    const int np = (int)max((int64_t)1, min(share, (int64_t)(s / kMinPart)));
-    p.tiles[k].parts = np;
-    far = max(far, (s + np - 1) / np);
-    if (np > 1) {
-      parts += np;
-      ++cut;
-    }
+  for (int k = tid; k < n; k += nt) {
+    const int s = k == tid ? first.n_sub : tiles[k].n_sub, np = share(s);
+    far = max(far, length(s, np));
+    v[0] += np > 1 ? np : 0;
+    v[1] += np > 1;
   }
-  atomicMax(&longest, far);
-  __syncthreads();
-  const int most = longest;
-  for (int k = r0; k < r1; ++k) {
-    const int s = p.tiles[k].n_sub, np = p.tiles[k].parts;
-    atomicAdd(&bucket[NB - 1 - (int)((int64_t)((s + np - 1) / np) * (NB - 1) / most)], np);
+  if (far > 1) atomicMax(&longest, far);
+  block_exclusive_scan_n<2>(v, ex, tot, sm);
+  const float scale = (float)(NB - 1) / (float)longest;
+  auto bucket_of = [&](int len) { return NB - 1 - min(NB - 1, (int)((float)len * scale)); };
+  for (int k = tid; k < n; k += nt) {
+    const int s = k == tid ? first.n_sub : tiles[k].n_sub, np = share(s);
+    atomicAdd(&bucket[bucket_of(length(s, np))], np);
   }
-  int64_t n_parts, n_cut;
-  int64_t part0 = block_exclusive_scan(parts, sm, &n_parts);
-  int64_t cut0 = block_exclusive_scan(cut, sm, &n_cut);
   __syncthreads();
   if (tid < kWave) {
     int base = 0;
     for (int b = 0; b < NB; b += kWave) {
-      const int v = bucket[b + tid];
-      const int inc = wave_inclusive_scan(v);
-      bucket[b + tid] = base + inc - v;
+      const int c = bucket[b + tid];
+      const int inc = wave_inclusive_scan(c);
+      bucket[b + tid] = base + inc - c;
       base += lane_value(inc, kWave - 1);
     }
     if (tid == 0) bucket[NB] = base;
   }
   __syncthreads();
   const int units = bucket[NB];
-  __syncthreads();
-  for (int k = r0; k < r1; ++k) {
-    const Tile tl = p.tiles[k];
-    const int s = tl.n_sub, np = tl.parts;
-    const int len = (s + np - 1) / np;
-    const int b = NB - 1 - (int)((int64_t)len * (NB - 1) / most);
-    if (np > 1) {
-      p.tiles[k].part0 = (int32_t)part0;
-      if (cut0 < target) p.split[cut0] = k;
-      ++cut0;
+  for (int k0 = tid - lane; k0 < n; k0 += nt) {      // a wave's 64 tiles
+    const int k = k0 + lane;
+    Tile tl = none;
+    int np = 0, u0 = 0, part0 = 0;
+    if (k < n) {
+      tl = k == tid ? first : tiles[k];
+      np = share(tl.n_sub);
+      u0 = atomicAdd(&bucket[bucket_of(length(tl.n_sub, np))], np);
+      part0 = (int)ex[0];
+      if (np > 1) {
+        if (ex[1] < target) p.split[ex[1]] = int4{tl.t0, tl.nt, part0, np};
+        ++ex[1];
+        ex[0] += np;
+      } else if (u0 < p.units_cap) {
+        p.units[u0] = Unit{tl.t0, tl.nt, tl.n_ent, -1, 0, tl.n_sub, entry_base(k, tl.e0)};
+      }
     }
-    const int u0 = atomicAdd(&bucket[b], np);
-    for (int x = 0; x < np; ++x) {
-      // even parts of whole steps where they are long
-      const int a = (int)((int64_t)s * x / np), z = (int)((int64_t)s * (x + 1) / np);
-      if (u0 + x < p.units_cap)
-        p.units[u0 + x] = Unit{tl.t0, tl.nt, tl.n_ent, np > 1 ? (int32_t)part0 + x : -1, a, z,
-                               entry_base(k, tl.e0)};
+    for (uint64_t cut = ballot(np > 1); cut; cut &= cut - 1) {      // a wave lists the parts
+      const int j = __builtin_ctzll(cut);
+      const int m = lane_value(np, j), u = lane_value(u0, j), s = lane_value(tl.n_sub, j);
+      const int len = s / m, more = s % m;           // the first `more` parts have one more
+      const Unit base{lane_value(tl.t0, j), lane_value(tl.nt, j), lane_value(tl.n_ent, j),
+                      lane_value(part0, j), 0, 0, entry_base(k0 + j, lane_value(tl.e0, j))};
+      for (int x = lane; x < m; x += kWave)
+        if (u + x < p.units_cap)
+          p.units[u + x] = Unit{base.t0, base.nt, base.n_ent, base.part + x,
+                                len * x + min(x, more), len * (x + 1) + min(x + 1, more),
+                                base.ent};
     }
-    if (np > 1) part0 += np;
   }
   if (tid == 0) {
     p.head->n_units = units;
-    p.head->n_split = (int)n_cut;
-    if (units > p.units_cap || n_cut > target) status_error(status, ARBOR_ECORRUPT);
+    p.head->n_split = (int)tot[1];
+    if (units > p.units_cap || tot[1] > target) status_error(status, ARBOR_ECORRUPT);
     else p.head->magic = kMagic;
   }
+}
+
+// The whole plan of a call with few blocks and tiles, in one launch: a wave walks all
+// chains beside one that cuts the tiles, then 16 waves merge them.  What bounds it is the
+// latency of one load after the other, so ids of parents, cu and tiles are in LDS.
+constexpr int kSmallTiles = 130, kSmallV = 8192;
+__global__ __launch_bounds__(1024) void plan_small(Tree t, int G, int Hkv, int P,
+                                                   const int32_t *__restrict__ nodes, int n_seq,
+                                                   const int32_t *__restrict__ cu, int n_tokens,
+                                                   PlanPtrs p, int target, int min_part, int32_t *status) {
+  __shared__ int32_t chain[MAXD * kCol], depth[kWave], sh_cu[kWave + 1], sh_parent[kSmallV];
+  __shared__ Tile tiles[kSmallTiles];
+  __shared__ int n_tiles;
+  const int wave = threadIdx.x >> 6, lane = lane_id();
+  const int leaf = wave == 1 && lane < n_seq ? nodes[lane] : -1;
+  for (int i = threadIdx.x; i < t.V; i += 1024) sh_parent[i] = t.parent[i];
+  if (threadIdx.x == 0) p.head->magic = 0;
+  if (status_failed(status)) return;
+  if (!request_ok(t, nodes, n_seq, cu, n_tokens, sh_cu)) {
+    if (threadIdx.x == 0) status_error(status, ARBOR_EINVAL);
+    return;
+  }
+  int err = 0;
+  if (wave == 0) {
+    const int n = cut_tiles(G, n_seq, sh_cu, tiles, kSmallTiles, status);
+    if (lane == 0) n_tiles = n;
+  } else if (wave == 1) {
+    const int d = walk_chain(sh_parent, leaf, chain, lane);
+    depth[lane] = d;
+    err = d < 0 ? d : 0;
+  }
+  if (__syncthreads_or(err)) {
+    if (err) status_error(status, err);
+    return;
+  }
+  for (int k = wave; k < n_tiles; k += 16) {
+    const int col = min(tiles[k].e0 + lane, kWave - 1);
+    merge_chains(t, sh_cu, p, k, &tiles[k], chain, col, depth[col]);
+  }
+  if (threadIdx.x == 0) write_header(p, t.V, G, Hkv, P, n_seq, n_tokens, n_tiles);
+  __syncthreads();
+  list_units(p, tiles, n_tiles, target, min_part, status);
+}
+
+// The same in three launches: tiles, a wave for each tile's chains, parts.
+constexpr int kCuLds = 4096;
+__global__ __launch_bounds__(1024) void plan_tiles(Tree t, int G, int Hkv, int P,
+                                                   const int32_t *__restrict__ nodes, int n_seq,
+                                                   const int32_t *__restrict__ cu, int n_tokens,
+                                                   PlanPtrs p, int32_t *status) {
+  __shared__ int32_t sh_cu[kCuLds + 1];
+  if (threadIdx.x == 0) p.head->magic = 0;
+  if (status_failed(status)) return;
+  const bool in_lds = n_seq <= kCuLds;
+  if (!request_ok(t, nodes, n_seq, cu, n_tokens, in_lds ? sh_cu : nullptr)) {
+    if (threadIdx.x == 0) status_error(status, ARBOR_EINVAL);
+    return;
+  }
+  if (threadIdx.x >= kWave) return;
+  const int n = in_lds ? cut_tiles(G, n_seq, sh_cu, p.tiles, (int)p.tiles_cap, status)
+                       : cut_tiles(G, n_seq, cu, p.tiles, (int)p.tiles_cap, status);
+  if (threadIdx.x == 0) write_header(p, t.V, G, Hkv, P, n_seq, n_tokens, n);
+}
+__global__ __launch_bounds__(64) void plan_chains(Tree t, const int32_t *__restrict__ nodes,
+                                                  const int32_t *__restrict__ cu, PlanPtrs p,
+                                                  int32_t *status) {
+  __shared__ int32_t chain[MAXD * kCol];
+  if (status_failed(status) || (int)blockIdx.x >= p.head->n_tiles) return;
+  const int lane = lane_id(), e0 = p.tiles[blockIdx.x].e0, ne = p.tiles[blockIdx.x].ne;
+  const int d = walk_chain(t.parent, lane < ne ? nodes[e0 + lane] : -1, chain, lane);
+  if (d < 0) status_error(status, d);
+  if (ballot(d < 0)) return;
+  merge_chains(t, cu, p, blockIdx.x, &p.tiles[blockIdx.x], chain, lane, d);
+}
+__global__ __launch_bounds__(1024) void plan_units(PlanPtrs p, int target, int min_part,
+                                                   int32_t *status) {
+  if (status_failed(status)) return;
+  list_units(p, p.tiles, p.head->n_tiles, target, min_part, status);
 }
 
 // ---- attention -------------------------------------------------------------------
@@ -376,7 +463,7 @@ struct Cfg {
   static constexpr int ES = (int)sizeof(T);
   static constexpr int ROW = D * ES;                     // bytes of a row
   static constexpr int PIECES = ROW / 16;
-  static constexpr int SUBS = ES == 2 ? 4 : 2;           // sub-pages of a step
+  static constexpr int SUBS = step_subs(ES);           // sub-pages of a step
   static constexpr int KEYS = 16 * SUBS;
   static constexpr int NS = KEYS / 32;                   // 32-key tiles of S
   static constexpr int BUF = KEYS * ROW;                 // K (or V) of a step
@@ -806,10 +893,9 @@ __global__ __launch_bounds__(kRows * 2, 2) void prefill_attn(AttnArgs a) {
         if (mask) {
           hidden = hide(z, cur, st, kt);
           masked = __builtin_amdgcn_readfirstlane(1);
-        } else {
-          all_set = __builtin_amdgcn_readfirstlane(1);
         }
         raise(z);
+        all_set = __builtin_amdgcn_readfirstlane(ballot(ref == -INFINITY) == 0);
       }
       Terms t = terms(z, base);
       check(t, z);
@@ -855,16 +941,21 @@ __global__ __launch_bounds__(kRows * 2, 2) void prefill_attn(AttnArgs a) {
     base = l = 0.0f;
     all_set = masked = 0;
   };
-  // A step in which every row has a reference and sees every key: its logits, then the next
+  // A step in which every row has a reference: its logits, then the next
   // step's loads (issued before them, their writes to LDS hold up the reads of K: 8,192
   // tokens of the 70B shape 1,137 us, now 1,094), then the terms and products of one half
   // after the other, V operands read three products ahead.
-  auto common_step = [&](int at, auto more) __attribute__((always_inline)) {
+  auto common_step = [&](int st, int at, bool mask, auto more) __attribute__((always_inline)) {
     if constexpr (sizeof(T) == 2) {
       constexpr int NV = 2 * C::DT, AHEAD = 3;           // V operands of a half
       f32x16 z0 = logits(at, 0), z1 = logits(at, 1);
       fence_order();
       more();
+      if (mask) {
+        hide(z0, win, st, 0);
+        hide(z1, win, st, 1);
+        masked = __builtin_amdgcn_readfirstlane(1);
+      }
       bf16x8 v[AHEAD + 1];
 #pragma unroll
       for (int j = 0; j < AHEAD; ++j) v[j] = values(at, j / C::DT, j % C::DT);
@@ -885,9 +976,13 @@ __global__ __launch_bounds__(kRows * 2, 2) void prefill_attn(AttnArgs a) {
         t = u;
       }
     } else {
-      const f32x16 z = logits(at, 0);
+      f32x16 z = logits(at, 0);
       fence_order();
       more();
+      if (mask) {
+        hide(z, win, st, 0);
+        masked = __builtin_amdgcn_readfirstlane(1);
+      }
       Terms t = terms(z, base);
       check(t, z);
       add(t, at, 0);
@@ -911,11 +1006,10 @@ __global__ __launch_bounds__(kRows * 2, 2) void prefill_attn(AttnArgs a) {
       none &= inf;
     }
     const bool some = any_live && !none;
-    const bool common = some && __builtin_amdgcn_readfirstlane(all_set) &&
-                        !(flags & (kMask | kNone));
+    const bool common = some && __builtin_amdgcn_readfirstlane(all_set);
     if (!common) more();
     if (some && !common) plain_step(win, st, at, std::false_type{});
-    if (common) common_step(at, more);
+    if (common) common_step(st, at, (flags & (kMask | kNone)) != 0, more);
     if (ws + 1 == WSTEPS) win = nxt;
     at ^= C::BUF;
   }
@@ -976,42 +1070,69 @@ __global__ __launch_bounds__(kRows * 2, 2) void prefill_attn(AttnArgs a) {
   }
 }
 
-// Joins the parts of the tiles that have several: a workgroup per 16 rows of a tile
-// and KV head, D / 4 lanes a row, parts in order.
+// Joins the parts of the tiles that have several: a workgroup per 8 or 16 rows of a tile
+// and KV head, D / 4 lanes a row, parts in order.  It waits on memory, not for much of it:
+// a row's references come in one load of its lanes, one part each, and the first parts'
+// sums are on their way before these are there.
 template <class T, int D>
 __global__ __launch_bounds__(256) void prefill_join(AttnArgs a) {
-  if (status_failed(a.status) || !header_ok(a)) return;
-  constexpr int LPR = D / 4, RPW = 256 / LPR, NG = kRows / RPW;
+  constexpr int LPR = D / 4, RPW = 256 / LPR, NG = kRows / RPW, U = 4;
   const Pool &pl = a.pl;
   int x = blockIdx.x;
   const int grp = x % NG;
   x /= NG;
   const int g = x % pl.Hkv, k = x / pl.Hkv;
-  if (k >= a.p.head->n_split) return;
-  const Tile tl = a.p.tiles[a.p.split[k]];
-  const int row = grp * RPW + threadIdx.x / LPR, c = threadIdx.x % LPR * 4;
-  const int tq = row / pl.G;
-  if (tq >= tl.nt || tl.part0 + tl.parts > a.part_cap) return;
+  const int4 tl = a.p.split[min(k, target_parts(pl.Hkv) - 1)];
+  const bool failed = status_failed(a.status), ok = header_ok(a);
+  if (failed || !ok || k >= a.p.head->n_split) return;
+  const int t0 = tl.x, nt = tl.y, part0 = tl.z, parts = tl.w;
+  if (grp * RPW / pl.G >= nt || part0 + parts > a.part_cap) return;
+  const int row = grp * RPW + threadIdx.x / LPR, lane = threadIdx.x % LPR, c = lane * 4;
   const int64_t stride = (int64_t)pl.Hkv * kRows * (D + 4);
-  const float *pp = a.part + (((int64_t)tl.part0 * pl.Hkv + g) * kRows + row) * (D + 4);
-  float m = -INFINITY;
-  for (int e = 0; e < tl.parts; ++e) m = fmaxf(m, pp[e * stride + D]);
+  const float *pp = a.part + (((int64_t)part0 * pl.Hkv + g) * kRows + row) * (D + 4);
+  f32x4 v[U];
+  auto load = [&](int e0) {
+#pragma unroll
+    for (int i = 0; i < U; ++i)
+      v[i] = *reinterpret_cast<const f32x4 *>(pp + min(e0 + i, parts - 1) * stride + c);
+  };
+  load(0);
+  typedef float f32x2 __attribute__((ext_vector_type(2)));
+  auto sums = [&](int e) {                 // reference and sum of one part
+    return e < parts ? *reinterpret_cast<const f32x2 *>(pp + e * stride + D)
+                     : f32x2{-INFINITY, 0.0f};
+  };
+  f32x2 rs = sums(lane);
+  float m = rs[0];
+  for (int e = lane + LPR; e < parts; e += LPR) m = fmaxf(m, sums(e)[0]);
+#pragma unroll
+  for (int y = 1; y < LPR; y *= 2) m = fmaxf(m, __shfl_xor(m, y));
   const float base = m == -INFINITY ? 0.0f : m;
   float l = 0.0f;
   f32x4 o = {0.0f, 0.0f, 0.0f, 0.0f};
-  for (int e = 0; e < tl.parts; ++e) {
-    const float *q = pp + e * stride;
-    const float ref = q[D];
+  for (int e0 = 0; e0 < parts; e0 += LPR) {
+    if (e0) rs = sums(e0 + lane);
     // a part whose terms have no reference holds sums of 0 (or NaN, which stays)
-    const float w = ref == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(ref - base);
-    l += w * q[D + 1];
-    const f32x4 v = *reinterpret_cast<const f32x4 *>(q + c);
+    const float w = rs[0] == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(rs[0] - base);
+    l += w * rs[1];
+    for (int e = e0; e < min(e0 + LPR, parts); e += U) {
+      if (e) load(e);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) o[i] += w * v[i];
+      for (int i = 0; i < U; ++i) {
+        const float we = __shfl(w, (e - e0) + i, LPR);
+        if (e + i < parts)
+#pragma unroll
+          for (int y = 0; y < 4; ++y) o[y] += we * v[i][y];
+      }
+    }
   }
+#pragma unroll
+  for (int y = 1; y < LPR; y *= 2) l += __shfl_xor(l, y);
+  const int tq = row / pl.G;
+  if (tq >= nt) return;
   const float inv = l == 0.0f ? 0.0f : 1.0f / l;
   const int Hq = pl.Hkv * pl.G, head = g * pl.G + row - tq * pl.G;
-  const int64_t tok = tl.t0 + tq;
+  const int64_t tok = t0 + tq;
   typedef T ovec __attribute__((ext_vector_type(4)));
   ovec w;
 #pragma unroll
@@ -1052,12 +1173,22 @@ int launch_prefill_plan(const arbor_geom_t *geom, const arbor_tree_t *tree, cons
   const PlanPtrs p = carve_plan(geom, n_seq, n_tokens, plan, plan_bytes, nullptr);
   if (!p.head) return ARBOR_EWORKSPACE;
   const Tree t = make_tree(tree);
-  hipLaunchKernelGGL(plan_tiles, dim3(1), dim3(1024), 0, stream, t, geom->q_per_kv,
-                     geom->num_kv_heads, geom->page_size, nodes, n_seq, cu, n_tokens, p, status);
-  hipLaunchKernelGGL(plan_chains, dim3((unsigned)p.tiles_cap), dim3(64), 0, stream, t, nodes, cu, p,
-                     status);
-  hipLaunchKernelGGL(plan_units, dim3(1), dim3(1024), 0, stream, p,
-                     target_parts(geom->num_kv_heads), status);
+  const int G = geom->q_per_kv, Hkv = geom->num_kv_heads, P = geom->page_size;
+  const int target = target_parts(Hkv);
+  const int min_part = kMinSteps * step_subs(geom->dtype == ARBOR_BF16 ? 2 : 4);
+  // 16 waves take a few rounds over a few tiles; one block's 100 tiles and more are faster
+  // one wave each, as are the chains of more blocks than a wave has lanes
+  if (n_seq <= kMaxSeq && p.tiles_cap <= kSmallTiles && t.V <= kSmallV) {
+    hipLaunchKernelGGL(plan_small, dim3(1), dim3(1024), 0, stream, t, G, Hkv, P, nodes, n_seq, cu,
+                       n_tokens, p, target, min_part, status);
+  } else {
+    hipLaunchKernelGGL(plan_tiles, dim3(1), dim3(1024), 0, stream, t, G, Hkv, P, nodes, n_seq, cu,
+                       n_tokens, p, status);
+    hipLaunchKernelGGL(plan_chains, dim3((unsigned)p.tiles_cap), dim3(64), 0, stream, t, nodes, cu,
+                       p, status);
+    hipLaunchKernelGGL(plan_units, dim3(1), dim3(1024), 0, stream, p, target, min_part,
+                       status);
+  }
   return hip_ok(hipGetLastError());
 }
 
@@ -1085,7 +1216,8 @@ int launch_prefill(const arbor_geom_t *geom, const arbor_tree_t *tree, const arb
   a.status = status;
   const int target = target_parts(geom->num_kv_heads);
   const int64_t units = a.p.units_cap * geom->num_kv_heads;
-  const int64_t tiles = a.p.tiles_cap < target ? a.p.tiles_cap : target;
+  // tiles of two parts or more
+  const int64_t split = a.p.tiles_cap < target / 2 ? a.p.tiles_cap : target / 2;
   if (units > INT32_MAX) return ARBOR_EUNSUPPORTED;
 #define ARBOR_PREFILL_LAUNCH(T, D)                                                             \
   do {                                                                                         \
@@ -1093,9 +1225,10 @@ int launch_prefill(const arbor_geom_t *geom, const arbor_tree_t *tree, const arb
     hipLaunchKernelGGL((prefill_attn<T, D>), dim3((unsigned)units), dim3(kRows * 2),           \
                        (Cfg<T, D>::LDS), stream, a);                                           \
     timing_end(geom, ARBOR_KERNEL_PREFILL_ATTN, stream);                                       \
-    hipLaunchKernelGGL((prefill_join<T, D>),                                                   \
-                       dim3((unsigned)(tiles * geom->num_kv_heads * (kRows * D / 4 / 256))),   \
-                       dim3(256), 0, stream, a);                                               \
+    if (split > 0)                                                                             \
+      hipLaunchKernelGGL((prefill_join<T, D>),                                                 \
+                         dim3((unsigned)(split * geom->num_kv_heads * (kRows * D / 4 / 256))), \
+                         dim3(256), 0, stream, a);                                             \
   } while (0)
   if (geom->dtype == ARBOR_BF16) {
     if (geom->head_dim == 128) ARBOR_PREFILL_LAUNCH(__bf16, 128);
