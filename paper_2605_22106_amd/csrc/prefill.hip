@@ -149,44 +149,53 @@ __device__ bool request_ok(const Tree &t, const int32_t *__restrict__ nodes, int
   return !__syncthreads_or(err);
 }
 
-// Cuts the packed tokens into tiles; one wave.  A tile takes the next block's tokens when
-// all of them fit (two blocks in one tile read the blocks that they share once, and
-// nothing twice); a block of more tokens than a tile holds starts its own.  The wave goes
-// from tile to tile, 64 blocks at a time in its lanes.  Returns how many tiles there are.
+// Cuts the packed tokens into tiles; one wave.  A tile takes the next blocks' tokens as
+// long as all of a block's fit (two blocks in one tile read the blocks that they share once,
+// and nothing twice); a block of more tokens than a tile holds starts its own.  From where a
+// tile starts with a block follows where the next one does: lanes find that for 64 blocks at
+// a time, and the wave follows these links from the first block on.  Returns how many tiles
+// there are.
 __device__ int cut_tiles(int G, int n_seq, const int32_t *cu, Tile *tiles, int tiles_cap,
                          int32_t *status) {
   const int lane = lane_id(), TQ = tokens_per_tile(G);
-  int e = 0, off = 0, k = 0;               // off: tokens of sequence e already in tiles
-  while (e < n_seq) {
-    const int c0 = e + lane < n_seq ? cu[e + lane] : 0;
-    const int c1 = e + lane < n_seq ? cu[e + lane + 1] : 0;
-    const int m = e + lane < n_seq ? c1 - c0 - (lane == 0 ? off : 0) : TQ + 1;
-    const int first = lane_value(m, 0), t0 = lane_value(c0, 0) + off;
-    if (first == 0) {
-      const uint64_t some = ballot(m != 0);
-      e += some ? __builtin_ctzll(some) : kWave;
-      off = 0;
-      continue;
-    }
-    if (first > TQ) {
-      const int full = first / TQ;
-      for (int x = lane; x < full; x += kWave)
-        if (k + x < tiles_cap) tiles[k + x] = Tile{t0 + x * TQ, TQ, e, 1, 0, 0};
-      k += full;
-      off += full * TQ;
-      if (full * TQ == first) {
-        ++e;
-        off = 0;
+  int k = 0, at = 0;                       // at: the block that the next tile starts with
+  for (int e0 = 0; e0 < n_seq; e0 += kWave) {
+    const int e = e0 + lane;
+    int c0 = 0, full = 0, t = 0, nt = 0, next = e + 1;
+    if (e < n_seq) {
+      c0 = cu[e];
+      const int m = cu[e + 1] - c0;
+      full = m / TQ;                       // whole tiles of this block alone
+      t = c0 + full * TQ;
+      if (m > full * TQ) {                 // the rest of it, and the blocks that fit
+        int hi = min(n_seq, e + kMaxSeq);  // last next with cu[next] <= t + TQ
+        while (next < hi) {
+          const int mid = (next + hi + 1) / 2;
+          if (cu[mid] <= t + TQ) next = mid;
+          else hi = mid - 1;
+        }
+        nt = cu[next] - t;
       }
-      continue;
     }
-    const int sum = wave_inclusive_scan(min(m, TQ + 1));
-    const int fit = popc(ballot(sum <= TQ));          // sums ascend
-    const int nt = lane_value(sum, fit - 1);
-    if (lane == 0 && k < tiles_cap) tiles[k] = Tile{t0, nt, e, fit, 0, 0};
-    ++k;
-    e += fit;
-    off = 0;
+    uint64_t path = 0;
+    while (at < min(e0 + kWave, n_seq)) {
+      path |= 1ull << (at - e0);
+      at = lane_value(next, at - e0);
+    }
+    const bool on = path >> lane & 1;
+    const int mine = on ? full + (nt > 0) : 0;
+    const int inc = wave_inclusive_scan(mine), k0 = k + inc - mine;
+    constexpr int FEW = 4;                 // tiles that a lane lists by itself
+    for (int x = 0; x < FEW; ++x)
+      if (on && x < full && k0 + x < tiles_cap) tiles[k0 + x] = Tile{c0 + x * TQ, TQ, e, 1, 0, 0};
+    for (uint64_t s = ballot(on && full > FEW); s; s &= s - 1) {
+      const int j = __builtin_ctzll(s), c = lane_value(c0, j), f = lane_value(full, j),
+                b = lane_value(k0, j);
+      for (int x = FEW + lane; x < f; x += kWave)
+        if (b + x < tiles_cap) tiles[b + x] = Tile{c + x * TQ, TQ, e0 + j, 1, 0, 0};
+    }
+    if (on && nt > 0 && k0 + full < tiles_cap) tiles[k0 + full] = Tile{t, nt, e, next - e, 0, 0};
+    k += lane_value(inc, kWave - 1);
   }
   if (k > tiles_cap) {                                // (the bound holds)
     if (lane == 0) status_error(status, ARBOR_ECORRUPT);
@@ -209,11 +218,12 @@ __device__ void write_header(const PlanPtrs &p, int V, int G, int Hkv, int P, in
 constexpr int kCol = kWave + 1;          // chains lie side by side, [MAXD][kCol], leaf first
 
 // The chain of the block x (none for x < 0) into column col: its length, or an error code.
-__device__ int walk_chain(const int32_t *parent, int x, int32_t *chain, int col) {
+template <class C>
+__device__ int walk_chain(const int32_t *parent, int x, C *chain, int col) {
   int depth = 0;
   while (x >= 0) {
     if (depth == MAXD) return ARBOR_EUNSUPPORTED;
-    chain[depth * kCol + col] = x;
+    chain[depth * kCol + col] = (C)x;
     ++depth;
     const int up = parent[x];
     if (up >= x) return ARBOR_EINVAL;
@@ -225,8 +235,10 @@ __device__ int walk_chain(const int32_t *parent, int x, int32_t *chain, int col)
 // Tile k's chain blocks, and its tokens' own slots; one wave.  Lane j's sequence has its
 // chain, `depth` blocks, in column col.  Blocks come in ascending order of ids, so the next
 // one is the smallest id that any lane has next; 64 of them wait in the lanes.
-__device__ void merge_chains(const Tree &t, const int32_t *cu, const PlanPtrs &p, int k,
-                             Tile *tile, const int32_t *chain, int col, int depth) {
+template <class C, class O>
+__device__ void merge_chains(const int32_t *n_kept, const O *page_off, const int32_t *cu,
+                             const PlanPtrs &p, int k, Tile *tile, const C *chain, int col,
+                             int depth) {
   const int lane = lane_id();
   const Tile tl = *tile;
   Entry *ents = p.ents + entry_base(k, tl.e0);
@@ -237,7 +249,7 @@ __device__ void merge_chains(const Tree &t, const int32_t *cu, const PlanPtrs &p
     hi = min(c1, tl.t0 + tl.nt);
     if (hi > lo) {
       leaf = chain[col];
-      newest = t.n_kept[leaf] - (c1 - hi) - 1;    // slot of the sequence's last token here
+      newest = n_kept[leaf] - (c1 - hi) - 1;    // slot of the sequence's last token here
     }
   }
   int subs = 0, n = 0;
@@ -245,8 +257,8 @@ __device__ void merge_chains(const Tree &t, const int32_t *cu, const PlanPtrs &p
   auto flush = [&](int cnt) {
     int need = 0;
     if (lane < cnt) {
-      if (mine.below != mine.own) mine.limit = t.n_kept[mine.node];
-      mine.po = (int32_t)t.page_off[mine.node];
+      if (mine.below != mine.own) mine.limit = n_kept[mine.node];
+      mine.po = (int32_t)page_off[mine.node];
       need = (mine.limit + 15) / 16;
     }
     const int inc = wave_inclusive_scan(need);
@@ -255,8 +267,17 @@ __device__ void merge_chains(const Tree &t, const int32_t *cu, const PlanPtrs &p
     subs += lane_value(inc, kWave - 1);
   };
   int at = leaf >= 0 ? depth - 1 : -1;
-  while (true) {
-    const int next = at >= 0 ? chain[at * kCol + col] : INT32_MAX;
+  if (tl.ne == 1) {                                // one chain: nothing to merge
+    n = lane_value(at, 0) + 1;
+    if (lane < n) {
+      mine.node = chain[(n - 1 - lane) * kCol + lane_value(col, 0)];
+      mine.limit = lane_value(newest, 0) + 1;
+      mine.below = 1;
+      mine.own = lane == n - 1;
+    }
+    if (n) flush(n);
+  } else while (true) {
+    const int next = at >= 0 ? (int)chain[at * kCol + col] : INT32_MAX;
     const int mn = wave_allreduce(next, [](int a, int b) { return a < b ? a : b; });
     if (mn == INT32_MAX) break;
     const bool here = next == mn;
@@ -273,7 +294,7 @@ __device__ void merge_chains(const Tree &t, const int32_t *cu, const PlanPtrs &p
     at -= here ? 1 : 0;
     if (++n % kWave == 0) flush(kWave);
   }
-  if (n % kWave) flush(n % kWave);
+  if (tl.ne > 1 && n % kWave) flush(n % kWave);
   if (lane == 0) {
     tile->n_ent = n;
     tile->n_sub = subs;
@@ -293,11 +314,13 @@ __device__ void list_units(const PlanPtrs &p, const Tile *tiles, int n, int targ
   constexpr int NB = 256;
   __shared__ int64_t sm[2 * 16];
   __shared__ int32_t bucket[NB + 1], longest;
-  const int nt = blockDim.x, tid = threadIdx.x, lane = lane_id();
+  // neighbouring tiles go to different waves: each wave has as many to list
+  const int nt = blockDim.x, lane = lane_id(), waves = nt / kWave;
+  const int tid = threadIdx.x, own = lane * waves + tid / kWave;
   const Tile none{};
-  const Tile first = tid < n ? tiles[tid] : none;
+  const Tile first = own < n ? tiles[own] : none;
   int64_t subs = 0;
-  for (int k = tid; k < n; k += nt) subs += k == tid ? first.n_sub : tiles[k].n_sub;
+  for (int k = own; k < n; k += nt) subs += k == own ? first.n_sub : tiles[k].n_sub;
   const int64_t total = block_sum(subs, sm);
   for (int b = tid; b <= NB; b += nt) bucket[b] = 0;
   if (tid == 0) longest = 1;
@@ -307,8 +330,8 @@ __device__ void list_units(const PlanPtrs &p, const Tile *tiles, int n, int targ
   auto length = [](int s, int np) { return (s + np - 1) / np; };
   int64_t v[2] = {0, 0}, ex[2], tot[2];        // parts of cut tiles, cut tiles
   int far = 0;
-  for (int k = tid; k < n; k += nt) {
-    const int s = k == tid ? first.n_sub : tiles[k].n_sub, np = share(s);
+  for (int k = own; k < n; k += nt) {
+    const int s = k == own ? first.n_sub : tiles[k].n_sub, np = share(s);
     far = max(far, length(s, np));
     v[0] += np > 1 ? np : 0;
     v[1] += np > 1;
@@ -317,8 +340,8 @@ __device__ void list_units(const PlanPtrs &p, const Tile *tiles, int n, int targ
   block_exclusive_scan_n<2>(v, ex, tot, sm);
   const float scale = (float)(NB - 1) / (float)longest;
   auto bucket_of = [&](int len) { return NB - 1 - min(NB - 1, (int)((float)len * scale)); };
-  for (int k = tid; k < n; k += nt) {
-    const int s = k == tid ? first.n_sub : tiles[k].n_sub, np = share(s);
+  for (int k = own; k < n; k += nt) {
+    const int s = k == own ? first.n_sub : tiles[k].n_sub, np = share(s);
     atomicAdd(&bucket[bucket_of(length(s, np))], np);
   }
   __syncthreads();
@@ -334,12 +357,12 @@ __device__ void list_units(const PlanPtrs &p, const Tile *tiles, int n, int targ
   }
   __syncthreads();
   const int units = bucket[NB];
-  for (int k0 = tid - lane; k0 < n; k0 += nt) {      // a wave's 64 tiles
-    const int k = k0 + lane;
+  for (int k0 = own - lane * waves; k0 < n; k0 += nt) {      // a wave's 64 tiles
+    const int k = k0 + lane * waves;
     Tile tl = none;
     int np = 0, u0 = 0, part0 = 0;
     if (k < n) {
-      tl = k == tid ? first : tiles[k];
+      tl = k == own ? first : tiles[k];
       np = share(tl.n_sub);
       u0 = atomicAdd(&bucket[bucket_of(length(tl.n_sub, np))], np);
       part0 = (int)ex[0];
@@ -356,7 +379,7 @@ __device__ void list_units(const PlanPtrs &p, const Tile *tiles, int n, int targ
       const int m = lane_value(np, j), u = lane_value(u0, j), s = lane_value(tl.n_sub, j);
       const int len = s / m, more = s % m;           // the first `more` parts have one more
       const Unit base{lane_value(tl.t0, j), lane_value(tl.nt, j), lane_value(tl.n_ent, j),
-                      lane_value(part0, j), 0, 0, entry_base(k0 + j, lane_value(tl.e0, j))};
+                      lane_value(part0, j), 0, 0, entry_base(k0 + j * waves, lane_value(tl.e0, j))};
       for (int x = lane; x < m; x += kWave)
         if (u + x < p.units_cap)
           p.units[u + x] = Unit{base.t0, base.nt, base.n_ent, base.part + x,
@@ -374,18 +397,24 @@ __device__ void list_units(const PlanPtrs &p, const Tile *tiles, int n, int targ
 
 // The whole plan of a call with few blocks and tiles, in one launch: a wave walks all
 // chains beside one that cuts the tiles, then 16 waves merge them.  What bounds it is the
-// latency of one load after the other, so ids of parents, cu and tiles are in LDS.
-constexpr int kSmallTiles = 130, kSmallV = 8192;
+// latency of one access after the other, so all that it reads twice is in LDS.
+constexpr int kSmallTiles = 130, kSmallV = 4096;
 __global__ __launch_bounds__(1024) void plan_small(Tree t, int G, int Hkv, int P,
                                                    const int32_t *__restrict__ nodes, int n_seq,
                                                    const int32_t *__restrict__ cu, int n_tokens,
                                                    PlanPtrs p, int target, int min_part, int32_t *status) {
-  __shared__ int32_t chain[MAXD * kCol], depth[kWave], sh_cu[kWave + 1], sh_parent[kSmallV];
+  __shared__ int32_t depth[kWave], sh_cu[kWave + 1];
+  __shared__ int32_t sh_parent[kSmallV], sh_kept[kSmallV], sh_page_off[kSmallV];
+  __shared__ uint16_t chain[MAXD * kCol];
   __shared__ Tile tiles[kSmallTiles];
   __shared__ int n_tiles;
   const int wave = threadIdx.x >> 6, lane = lane_id();
   const int leaf = wave == 1 && lane < n_seq ? nodes[lane] : -1;
-  for (int i = threadIdx.x; i < t.V; i += 1024) sh_parent[i] = t.parent[i];
+  for (int i = threadIdx.x; i < t.V; i += 1024) {
+    sh_parent[i] = t.parent[i];
+    sh_kept[i] = t.n_kept[i];
+    sh_page_off[i] = (int32_t)t.page_off[i];
+  }
   if (threadIdx.x == 0) p.head->magic = 0;
   if (status_failed(status)) return;
   if (!request_ok(t, nodes, n_seq, cu, n_tokens, sh_cu)) {
@@ -407,7 +436,7 @@ __global__ __launch_bounds__(1024) void plan_small(Tree t, int G, int Hkv, int P
   }
   for (int k = wave; k < n_tiles; k += 16) {
     const int col = min(tiles[k].e0 + lane, kWave - 1);
-    merge_chains(t, sh_cu, p, k, &tiles[k], chain, col, depth[col]);
+    merge_chains(sh_kept, sh_page_off, sh_cu, p, k, &tiles[k], chain, col, depth[col]);
   }
   if (threadIdx.x == 0) write_header(p, t.V, G, Hkv, P, n_seq, n_tokens, n_tiles);
   __syncthreads();
@@ -442,7 +471,7 @@ __global__ __launch_bounds__(64) void plan_chains(Tree t, const int32_t *__restr
   const int d = walk_chain(t.parent, lane < ne ? nodes[e0 + lane] : -1, chain, lane);
   if (d < 0) status_error(status, d);
   if (ballot(d < 0)) return;
-  merge_chains(t, cu, p, blockIdx.x, &p.tiles[blockIdx.x], chain, lane, d);
+  merge_chains(t.n_kept, t.page_off, cu, p, blockIdx.x, &p.tiles[blockIdx.x], chain, lane, d);
 }
 __global__ __launch_bounds__(1024) void plan_units(PlanPtrs p, int target, int min_part,
                                                    int32_t *status) {
