@@ -95,6 +95,7 @@ __device__ __forceinline__ uint32_t ordered_key(float x) {
 namespace dpp {
 constexpr int kQuadXor1 = 0xB1;        // quad_perm [1,0,3,2]
 constexpr int kQuadXor2 = 0x4E;        // quad_perm [2,3,0,1]
+constexpr int kQuadMirror = 0x1B;      // quad_perm [3,2,1,0]
 constexpr int kRowHalfMirror = 0x141;  // lane i <- 7 - i within each 8
 constexpr int kRowMirror = 0x140;      // lane i <- 15 - i within each row
 constexpr int kRowShr = 0x110;         // + n: lane i <- i - n within the row
