@@ -538,10 +538,14 @@ struct AttnArgs {
   void *out;
   float *lse;
   float sl2;            // softmax scale in log2 units
-  float *part;          // [parts][Hkv][kRows][D + 2]
+  float *part;          // [parts][Hkv][kWaves][part_floats]
   int64_t part_cap;     // parts that it holds
   int32_t *status;
 };
+
+// Floats of a wave's rows in a part: their sums, then their references and sums of terms.
+template <int D>
+__host__ __device__ constexpr int part_floats() { return 32 * (D + 2); }
 
 // Direct loads to LDS of the rows of one sub-page, `bytes` of which are valid: 16
 // bytes a lane, load c from (off ^ (c FLIP & MASK)) + 1024 c to dst + 1024 c.  The buffer
@@ -970,16 +974,12 @@ __global__ __launch_bounds__(kRows * 2, 2) void prefill_attn(AttnArgs a) {
     base = l = 0.0f;
     all_set = masked = 0;
   };
-  // A step in which every row has a reference: its logits, then the next
-  // step's loads (issued before them, their writes to LDS hold up the reads of K: 8,192
-  // tokens of the 70B shape 1,137 us, now 1,094), then the terms and products of one half
-  // after the other, V operands read three products ahead.
-  auto common_step = [&](int st, int at, bool mask, auto more) __attribute__((always_inline)) {
+  // A step in which every row has a reference: the logits of both halves, then the terms and
+  // products of one half after the other, V operands read three products ahead.
+  auto common_step = [&](int st, int at, bool mask) __attribute__((always_inline)) {
     if constexpr (sizeof(T) == 2) {
       constexpr int NV = 2 * C::DT, AHEAD = 3;           // V operands of a half
       f32x16 z0 = logits(at, 0), z1 = logits(at, 1);
-      fence_order();
-      more();
       if (mask) {
         hide(z0, win, st, 0);
         hide(z1, win, st, 1);
@@ -1006,8 +1006,6 @@ __global__ __launch_bounds__(kRows * 2, 2) void prefill_attn(AttnArgs a) {
       }
     } else {
       f32x16 z = logits(at, 0);
-      fence_order();
-      more();
       if (mask) {
         hide(z, win, st, 0);
         masked = __builtin_amdgcn_readfirstlane(1);
@@ -1024,9 +1022,7 @@ __global__ __launch_bounds__(kRows * 2, 2) void prefill_attn(AttnArgs a) {
     const int ws = st % WSTEPS;
     if (ws == 0 && st + WSTEPS < steps) nxt = fill((st + WSTEPS) * C::SUBS);
     landed_barrier();          // of this step; every wave is done with the other buffer
-    auto more = [&]() __attribute__((always_inline)) {
-      if (st + 1 < steps) issue(ws + 1 < WSTEPS ? win : nxt, st + 1, at ^ C::BUF);
-    };
+    if (st + 1 < steps) issue(ws + 1 < WSTEPS ? win : nxt, st + 1, at ^ C::BUF);
     int flags = 0, none = kNone;
 #pragma unroll
     for (int sb = 0; sb < C::SUBS; ++sb) {
@@ -1036,21 +1032,22 @@ __global__ __launch_bounds__(kRows * 2, 2) void prefill_attn(AttnArgs a) {
     }
     const bool some = any_live && !none;
     const bool common = some && __builtin_amdgcn_readfirstlane(all_set);
-    if (!common) more();
+    const bool mask = (flags & (kMask | kNone)) != 0;
     if (some && !common) plain_step(win, st, at, std::false_type{});
-    if (common) common_step(st, at, (flags & (kMask | kNone)) != 0, more);
+    if (common) common_step(st, at, mask);
     if (ws + 1 == WSTEPS) win = nxt;
     at ^= C::BUF;
   }
   // A key that a row may not see has p = 0, but 0 times an infinite or NaN value is not
   // 0.  So a unit that hid keys and whose outputs are not all finite runs once more, its
   // steps with hidden keys summed key by key, without them.
-  bool finite = true;
+  float odd = 0.0f;                            // NaN if some output is not finite
+  if (masked)
 #pragma unroll
-  for (int d = 0; d < C::DT; ++d)
+    for (int d = 0; d < C::DT; ++d)
 #pragma unroll
-    for (int r = 0; r < 16; ++r) finite = finite && __builtin_isfinite(o[d][r]);
-  if (__syncthreads_or(live && masked && !finite)) {
+      for (int r = 0; r < 16; ++r) odd = __builtin_fmaf(o[d][r], 0.0f, odd);
+  if (__syncthreads_or(live && odd != 0.0f)) {
     clear();
     for (int st = 0; st < steps; ++st) {
       win = fill(st / WSTEPS * kWave);
@@ -1065,24 +1062,24 @@ __global__ __launch_bounds__(kRows * 2, 2) void prefill_attn(AttnArgs a) {
     return;
   }
   const float lt = swap_halves_add(l);
-  if (!live) return;
   if (un.part >= 0) {
+    // a part's sums: 1 KB a register quad, rows side by side, and a reference and a sum a row
     if (un.part >= a.part_cap) return;         // (the plan's bound holds)
-    float *pp = a.part + (((int64_t)un.part * pl.Hkv + g) * kRows + row) * (D + 4);
+    float *pp = a.part + (((int64_t)un.part * pl.Hkv + g) * kWaves + wave) * part_floats<D>();
 #pragma unroll
     for (int d = 0; d < C::DT; ++d)
 #pragma unroll
       for (int r = 0; r < 16; r += 4)
-        *reinterpret_cast<f32x4 *>(pp + 32 * d + 2 * r + 4 * h) =
+        *reinterpret_cast<f32x4 *>(pp + ((d * 4 + r / 4) * kWave + lane) * 4) =
             f32x4{o[d][r], o[d][r + 1], o[d][r + 2], o[d][r + 3]};
-    if (h == 0) {
-      pp[D] = ref;
-      pp[D + 1] = lt;
-    }
+    pp[32 * D + lane] = h ? lt : ref;
     return;
   }
   const float inv = lt == 0.0f ? 0.0f : 1.0f / lt;
-  T *op = static_cast<T *>(a.out) + ((int64_t)tok * Hq + head) * D;
+  // Rows leave whole, 16 bytes a lane: through the wave's share of LDS, in which a row's
+  // 16-byte pieces are turned by its number so that 32 rows' writes spread over the banks
+  char *own = lds + wave * (32 * C::ROW);
+  constexpr int TURN = C::PIECES < 32 ? C::PIECES - 1 : 31;
   typedef T ovec __attribute__((ext_vector_type(4)));
 #pragma unroll
   for (int d = 0; d < C::DT; ++d)
@@ -1091,97 +1088,111 @@ __global__ __launch_bounds__(kRows * 2, 2) void prefill_attn(AttnArgs a) {
       ovec w;
 #pragma unroll
       for (int i = 0; i < 4; ++i) w[i] = (T)(o[d][r + i] * inv);
-      *reinterpret_cast<ovec *>(op + 32 * d + 2 * r + 4 * h) = w;
+      const int byte = (32 * d + 2 * r + 4 * h) * C::ES;
+      *reinterpret_cast<ovec *>(own + lr * C::ROW + ((byte / 16 ^ (lr & TURN)) * 16 + byte % 16)) = w;
     }
-  if (a.lse && h == 0) {
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+  constexpr int RPI = kWave / C::PIECES;       // rows that one store covers
+#pragma unroll
+  for (int x = 0; x < 32 / RPI; ++x) {
+    const int r = x * RPI + lane / C::PIECES, c = lane % C::PIECES;
+    const u32x4 w = *reinterpret_cast<const u32x4 *>(own + r * C::ROW + ((c ^ (r & TURN)) * 16));
+    const int y = wave * 32 + r, yq = y / G;
+    if (yq < un.nt)
+      *reinterpret_cast<u32x4 *>(static_cast<char *>(a.out) +
+                                 (((int64_t)(un.t0 + yq) * Hq + g * G + (y - yq * G)) * C::ROW +
+                                  c * 16)) = w;
+  }
+  if (a.lse && h == 0 && live) {
     const float rf = ref == -INFINITY && lt != 0.0f ? 0.0f : ref;
     a.lse[(int64_t)tok * Hq + head] = (rf + __builtin_amdgcn_logf(lt)) * kLn2;
   }
 }
 
-// Joins the parts of the tiles that have several: a workgroup per 8 or 16 rows of a tile
-// and KV head, D / 4 lanes a row, parts in order.  It waits on memory, not for much of it:
-// a row's references come in one load of its lanes, one part each, and the first parts'
-// sums are on their way before these are there.
+// Joins the parts of the tiles that have several: a workgroup per 32 rows of a tile and KV
+// head, whose waves take the register quads that the attention's lanes had, each lane four
+// columns of one row at a time, parts in order.  It waits on memory: the first parts' sums
+// are on their way before their references are there.
 template <class T, int D>
 __global__ __launch_bounds__(256) void prefill_join(AttnArgs a) {
-  constexpr int LPR = D / 4, RPW = 256 / LPR, NG = kRows / RPW, U = 4;
+  constexpr int U = 4, QUADS = D / 8;
   const Pool &pl = a.pl;
   int x = blockIdx.x;
-  const int grp = x % NG;
-  x /= NG;
+  const int rows = x % kWaves;                  // 32 rows: the wave that had them
+  x /= kWaves;
   const int g = x % pl.Hkv, k = x / pl.Hkv;
   const int4 tl = a.p.split[min(k, target_parts(pl.Hkv) - 1)];
   const bool failed = status_failed(a.status), ok = header_ok(a);
   if (failed || !ok || k >= a.p.head->n_split) return;
   const int t0 = tl.x, nt = tl.y, part0 = tl.z, parts = tl.w;
-  if (grp * RPW / pl.G >= nt || part0 + parts > a.part_cap) return;
-  const int row = grp * RPW + threadIdx.x / LPR, lane = threadIdx.x % LPR, c = lane * 4;
-  const int64_t stride = (int64_t)pl.Hkv * kRows * (D + 4);
-  const float *pp = a.part + (((int64_t)part0 * pl.Hkv + g) * kRows + row) * (D + 4);
-  f32x4 v[U];
+  if (rows * 32 / pl.G >= nt || part0 + parts > a.part_cap) return;
+  const int lane = lane_id(), wave = threadIdx.x / kWave, lr = lane & 31, h = lane >> 5;
+  const int64_t stride = (int64_t)pl.Hkv * kWaves * part_floats<D>();
+  const float *pp = a.part + (((int64_t)part0 * pl.Hkv + g) * kWaves + rows) * part_floats<D>();
+  constexpr int MINE = QUADS / 4;               // quads of a wave
+  f32x4 o[MINE], v[U][MINE];
+  float ref[U], sum[U];
   auto load = [&](int e0) {
 #pragma unroll
-    for (int i = 0; i < U; ++i)
-      v[i] = *reinterpret_cast<const f32x4 *>(pp + min(e0 + i, parts - 1) * stride + c);
-  };
-  load(0);
-  typedef float f32x2 __attribute__((ext_vector_type(2)));
-  auto sums = [&](int e) {                 // reference and sum of one part
-    return e < parts ? *reinterpret_cast<const f32x2 *>(pp + e * stride + D)
-                     : f32x2{-INFINITY, 0.0f};
-  };
-  f32x2 rs = sums(lane);
-  float m = rs[0];
-  for (int e = lane + LPR; e < parts; e += LPR) m = fmaxf(m, sums(e)[0]);
+    for (int i = 0; i < U; ++i) {
+      ref[i] = -INFINITY;
+      if (e0 + i >= parts) continue;
+      const float *q = pp + (e0 + i) * stride;
+      ref[i] = q[32 * D + lr];
+      sum[i] = q[32 * D + 32 + lr];
 #pragma unroll
-  for (int y = 1; y < LPR; y *= 2) m = fmaxf(m, __shfl_xor(m, y));
-  const float base = m == -INFINITY ? 0.0f : m;
-  float l = 0.0f;
-  f32x4 o = {0.0f, 0.0f, 0.0f, 0.0f};
-  for (int e0 = 0; e0 < parts; e0 += LPR) {
-    if (e0) rs = sums(e0 + lane);
-    // a part whose terms have no reference holds sums of 0 (or NaN, which stays)
-    const float w = rs[0] == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(rs[0] - base);
-    l += w * rs[1];
-    for (int e = e0; e < min(e0 + LPR, parts); e += U) {
-      if (e) load(e);
-#pragma unroll
-      for (int i = 0; i < U; ++i) {
-        const float we = __shfl(w, (e - e0) + i, LPR);
-        if (e + i < parts)
-#pragma unroll
-          for (int y = 0; y < 4; ++y) o[y] += we * v[i][y];
-      }
+      for (int j = 0; j < MINE; ++j)
+        v[i][j] = *reinterpret_cast<const f32x4 *>(q + ((wave * MINE + j) * kWave + lane) * 4);
     }
-  }
+  };
+  float m = -INFINITY, l = 0.0f;
 #pragma unroll
-  for (int y = 1; y < LPR; y *= 2) l += __shfl_xor(l, y);
-  const int tq = row / pl.G;
+  for (int j = 0; j < MINE; ++j) o[j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+  for (int e0 = 0; e0 < parts; e0 += U) {
+    load(e0);
+    float to = m;
+#pragma unroll
+    for (int i = 0; i < U; ++i) to = fmaxf(to, ref[i]);
+    const float base = to == -INFINITY ? 0.0f : to;
+    const float by = m == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m - base);
+    l *= by;
+#pragma unroll
+    for (int j = 0; j < MINE; ++j) o[j] *= by;
+    m = to;
+#pragma unroll
+    for (int i = 0; i < U; ++i)
+      if (e0 + i < parts) {
+        // a part whose terms have no reference holds sums of 0 (or NaN, which stays)
+        const float w = ref[i] == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(ref[i] - base);
+        l += w * sum[i];
+#pragma unroll
+        for (int j = 0; j < MINE; ++j) o[j] += w * v[i][j];
+      }
+  }
+  const int row = rows * 32 + lr, tq = row / pl.G;
   if (tq >= nt) return;
   const float inv = l == 0.0f ? 0.0f : 1.0f / l;
   const int Hq = pl.Hkv * pl.G, head = g * pl.G + row - tq * pl.G;
   const int64_t tok = t0 + tq;
   typedef T ovec __attribute__((ext_vector_type(4)));
-  ovec w;
 #pragma unroll
-  for (int i = 0; i < 4; ++i) w[i] = (T)(o[i] * inv);
-  *reinterpret_cast<ovec *>(static_cast<T *>(a.out) + (tok * Hq + head) * D + c) = w;
-  if (a.lse && c == 0)
+  for (int j = 0; j < MINE; ++j) {
+    ovec w;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) w[i] = (T)(o[j][i] * inv);
+    *reinterpret_cast<ovec *>(static_cast<T *>(a.out) + (tok * Hq + head) * D +
+                              (wave * MINE + j) * 8 + 4 * h) = w;
+  }
+  if (a.lse && wave == 0 && h == 0)
     a.lse[tok * Hq + head] = ((m == -INFINITY && l != 0.0f ? 0.0f : m) +
                               __builtin_amdgcn_logf(l)) * kLn2;
 }
 
-inline int64_t part_bound(const arbor_geom_t *g, int n_seq, int n_tokens) {
-  (void)n_seq;
-  (void)n_tokens;
-  return target_parts(g->num_kv_heads);          // (shares are rounded down)
+inline size_t tile_floats(const arbor_geom_t *g) {      // of a part, all KV heads
+  return (size_t)g->num_kv_heads * kRows * (g->head_dim + 2);
 }
-
-inline size_t part_floats(const arbor_geom_t *g) {
-  return (size_t)g->num_kv_heads * kRows * (g->head_dim + 4);
-}
-
 }  // namespace
 
 size_t prefill_plan_size(const arbor_geom_t *g, int32_t n_seq, int32_t n_tokens) {
@@ -1192,7 +1203,7 @@ size_t prefill_plan_size(const arbor_geom_t *g, int32_t n_seq, int32_t n_tokens)
 
 size_t prefill_workspace_size(const arbor_geom_t *g, int32_t n_seq, int32_t n_tokens) {
   if (n_tokens == 0) return 256;
-  return (size_t)part_bound(g, n_seq, n_tokens) * part_floats(g) * 4 + 256;
+  return (size_t)target_parts(g->num_kv_heads) * tile_floats(g) * 4 + 256;
 }
 
 int launch_prefill_plan(const arbor_geom_t *geom, const arbor_tree_t *tree, const int32_t *nodes,
@@ -1230,8 +1241,8 @@ int launch_prefill(const arbor_geom_t *geom, const arbor_tree_t *tree, const arb
   a.p = carve_plan(geom, n_seq, n_tokens, const_cast<void *>(plan), plan_bytes, nullptr);
   if (!a.p.head) return ARBOR_EWORKSPACE;
   Carve cv(workspace, workspace_bytes);
-  a.part_cap = part_bound(geom, n_seq, n_tokens);
-  a.part = cv.take<float>((size_t)a.part_cap * part_floats(geom));
+  a.part_cap = target_parts(geom->num_kv_heads);        // (shares are rounded down)
+  a.part = cv.take<float>((size_t)a.part_cap * tile_floats(geom));
   if (!cv.ok) return ARBOR_EWORKSPACE;
   a.t = make_tree(tree);
   a.pl = make_pool(geom, pool);
@@ -1256,7 +1267,7 @@ int launch_prefill(const arbor_geom_t *geom, const arbor_tree_t *tree, const arb
     timing_end(geom, ARBOR_KERNEL_PREFILL_ATTN, stream);                                       \
     if (split > 0)                                                                             \
       hipLaunchKernelGGL((prefill_join<T, D>),                                                 \
-                         dim3((unsigned)(split * geom->num_kv_heads * (kRows * D / 4 / 256))), \
+                         dim3((unsigned)(split * geom->num_kv_heads * kWaves)),                \
                          dim3(256), 0, stream, a);                                             \
   } while (0)
   if (geom->dtype == ARBOR_BF16) {
