@@ -6,7 +6,9 @@
 // fp32 angle is off by up to 4e-3), and their sines and cosines, rounded once, shared
 // through LDS; then every group of D / 8 lanes takes one head, eight elements a lane.
 // The sum of squares crosses the lanes by DPP; nothing but the angles goes through LDS,
-// and each element is read and written once: HBM-bound.
+// and each element is read and written once: HBM-bound.  The norm's factor comes last: a
+// bf16 element times its weight is exact in fp32, and the fewer roundings before the last
+// one, the fewer elements fall on its other side.
 //
 // Where a pair of the rotation lies in one lane's 16 bytes (neighbours) or in those of the
 // lane half a head further on (halves of a whole head), a lane takes eight elements in a
@@ -156,39 +158,40 @@ __global__ __launch_bounds__(256) void append_rows(AppendArgs args) {
           vb[e] = (float)yb[e];
         }
         const void *w = is_q ? a.q_norm : a.k_norm;
+        float r = 1.0f;
         if (w) {
           float ss = 0.0f;
 #pragma unroll
           for (int e = 0; e < 4; ++e) ss += va[e] * va[e] + vb[e] * vb[e];
           ss = row_sum<LPR>(ss);
-          const float r = 1.0f / sqrtf(ss * (1.0f / D) + a.eps);
+          r = 1.0f / sqrtf(ss * (1.0f / D) + a.eps);
           const reg wa = *reinterpret_cast<const reg *>(static_cast<const T *>(w) + ca);
           const reg wb = *reinterpret_cast<const reg *>(static_cast<const T *>(w) + cb);
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
-            va[e] *= r * (float)wa[e];
-            vb[e] *= r * (float)wb[e];
+            va[e] *= (float)wa[e];               // (exact for bf16)
+            vb[e] *= (float)wb[e];
           }
         }
         if (split) {
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
-            ya[e] = (T)(va[e] * co[e] - vb[e] * si[e]);
-            yb[e] = (T)(vb[e] * co[e] + va[e] * si[e]);
+            ya[e] = (T)(r * (va[e] * co[e] - vb[e] * si[e]));
+            yb[e] = (T)(r * (vb[e] * co[e] + va[e] * si[e]));
           }
         } else if (turns) {
 #pragma unroll
           for (int e = 0; e < 2; ++e) {
-            ya[2 * e] = (T)(va[2 * e] * co[e] - va[2 * e + 1] * si[e]);
-            ya[2 * e + 1] = (T)(va[2 * e + 1] * co[e] + va[2 * e] * si[e]);
-            yb[2 * e] = (T)(vb[2 * e] * co[2 + e] - vb[2 * e + 1] * si[2 + e]);
-            yb[2 * e + 1] = (T)(vb[2 * e + 1] * co[2 + e] + vb[2 * e] * si[2 + e]);
+            ya[2 * e] = (T)(r * (va[2 * e] * co[e] - va[2 * e + 1] * si[e]));
+            ya[2 * e + 1] = (T)(r * (va[2 * e + 1] * co[e] + va[2 * e] * si[e]));
+            yb[2 * e] = (T)(r * (vb[2 * e] * co[2 + e] - vb[2 * e + 1] * si[2 + e]));
+            yb[2 * e + 1] = (T)(r * (vb[2 * e + 1] * co[2 + e] + vb[2 * e] * si[2 + e]));
           }
         } else {
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
-            ya[e] = (T)va[e];
-            yb[e] = (T)vb[e];
+            ya[e] = (T)(r * va[e]);
+            yb[e] = (T)(r * vb[e]);
           }
         }
       }
@@ -299,25 +302,26 @@ __global__ __launch_bounds__(BLOCK, sizeof(T) == 2 ? 8 : 4) void append_whole(Ap
           p[e] = (float)far.e[HALVES ? e : e ^ 1];
         }
         const T *w = static_cast<const T *>(is_q ? a.q_norm : a.k_norm);
+        float r = 1.0f;
         if (w) {
           float ss = 0.0f;
 #pragma unroll
           for (int e = 0; e < 8; ++e) ss += v[e] * v[e];
           ss = row_sum<LPR>(ss);
-          const float r = 1.0f / sqrtf(ss * (1.0f / D) + a.eps);
+          r = 1.0f / sqrtf(ss * (1.0f / D) + a.eps);
           const int c = 8 * q8;
           const Eight wo = __builtin_bit_cast(Eight, *reinterpret_cast<const words *>(w + c));
           const Eight wf = __builtin_bit_cast(
               Eight, *reinterpret_cast<const words *>(w + (HALVES ? c ^ (D / 2) : c)));
 #pragma unroll
           for (int e = 0; e < 8; ++e) {
-            v[e] *= r * (float)wo.e[e];
-            p[e] *= r * (float)wf.e[HALVES ? e : e ^ 1];
+            v[e] *= (float)wo.e[e];              // (exact for bf16)
+            p[e] *= (float)wf.e[HALVES ? e : e ^ 1];
           }
         }
         Eight out;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) out.e[e] = (T)(turns ? v[e] * co[e] + p[e] * si[e] : v[e]);
+        for (int e = 0; e < 8; ++e) out.e[e] = (T)(r * (turns ? v[e] * co[e] + p[e] * si[e] : v[e]));
         y = __builtin_bit_cast(words, out);
       }
       T *out;
