@@ -638,11 +638,12 @@ int arbor_prefill_plan(const arbor_geom_t *geom, const arbor_tree_t *tree, const
  * over every resident slot of every proper ancestor of i and the slots of i up to
  * the token's own.  q and out [n_tokens][Hq][head_dim] in the pool's dtype, lse_out
  * [n_tokens][Hq] fp32 natural-log LSE (nullable); softmax_scale <= 0 means
- * 1/sqrt(head_dim).  The tokens of several blocks share the reads of the ancestors
- * that they have in common.  For bf16 pools the weights are rounded to bf16 before
- * their product with V (as V and the output are); all sums are fp32.  What a token
- * may not see (later tokens, other blocks, unused rows of a page) has no influence
- * on its output, infinities and NaN included.  Results are bitwise reproducible.
+ * 1/sqrt(head_dim).  out may be q itself.  The tokens of several blocks share the
+ * reads of the ancestors that they have in common.  For bf16 pools the weights are
+ * rounded to bf16 before their product with V (as V and the output are); all sums
+ * are fp32.  What a token may not see (later tokens, other blocks, unused rows of a
+ * page) has no influence on its output, infinities and NaN included.  Results are
+ * bitwise reproducible.  Calls that run at once may share a plan, not a workspace.
  * `plan` is arbor_prefill_plan's for this n_seq and n_tokens; `workspace` holds
  * arbor_prefill_workspace_size() bytes.
  * Errors: EINVAL (arguments, a plan of another call or of a tree that has changed

@@ -56,6 +56,7 @@ constexpr int kMinSteps = 2;
 struct Header {
   int64_t magic;
   int32_t n_seq, n_tokens, V, G, Hkv, page_size, n_tiles, n_units, n_split;
+  int64_t table;                 // entries of the page table
 };
 
 struct Tile {
@@ -204,11 +205,12 @@ __device__ int cut_tiles(int G, int n_seq, const int32_t *cu, Tile *tiles, int t
   return k;
 }
 
-__device__ void write_header(const PlanPtrs &p, int V, int G, int Hkv, int P, int n_seq,
+__device__ void write_header(const PlanPtrs &p, const Tree &t, int G, int Hkv, int P, int n_seq,
                              int n_tokens, int n_tiles) {
   p.head->n_seq = n_seq;
   p.head->n_tokens = n_tokens;
-  p.head->V = V;
+  p.head->V = t.V;
+  p.head->table = t.page_off[t.V];
   p.head->G = G;
   p.head->Hkv = Hkv;
   p.head->page_size = P;
@@ -438,7 +440,7 @@ __global__ __launch_bounds__(1024) void plan_small(Tree t, int G, int Hkv, int P
     const int col = min(tiles[k].e0 + lane, kWave - 1);
     merge_chains(sh_kept, sh_page_off, sh_cu, p, k, &tiles[k], chain, col, depth[col]);
   }
-  if (threadIdx.x == 0) write_header(p, t.V, G, Hkv, P, n_seq, n_tokens, n_tiles);
+  if (threadIdx.x == 0) write_header(p, t, G, Hkv, P, n_seq, n_tokens, n_tiles);
   __syncthreads();
   list_units(p, tiles, n_tiles, target, min_part, status);
 }
@@ -460,7 +462,7 @@ __global__ __launch_bounds__(1024) void plan_tiles(Tree t, int G, int Hkv, int P
   if (threadIdx.x >= kWave) return;
   const int n = in_lds ? cut_tiles(G, n_seq, sh_cu, p.tiles, (int)p.tiles_cap, status)
                        : cut_tiles(G, n_seq, cu, p.tiles, (int)p.tiles_cap, status);
-  if (threadIdx.x == 0) write_header(p, t.V, G, Hkv, P, n_seq, n_tokens, n);
+  if (threadIdx.x == 0) write_header(p, t, G, Hkv, P, n_seq, n_tokens, n);
 }
 __global__ __launch_bounds__(64) void plan_chains(Tree t, const int32_t *__restrict__ nodes,
                                                   const int32_t *__restrict__ cu, PlanPtrs p,
@@ -642,10 +644,13 @@ constexpr int kMask = 1 << 16;   // some row of this wave must not see some key 
 constexpr int kNone = 1 << 17;   // no row of this wave sees any
 static_assert(kMaxSeq * MAXD <= 4096, "chain blocks of a tile fit 12 bits");
 
+// (all in one round trip)
 __device__ __forceinline__ bool header_ok(const AttnArgs &a) {
-  const Header *h = a.p.head;
-  return h->magic == kMagic && h->n_seq == a.n_seq && h->n_tokens == a.n_tokens &&
-         h->V == a.t.V && h->G == a.pl.G && h->Hkv == a.pl.Hkv && h->page_size == a.pl.P;
+  const Header h = *a.p.head;
+  const int64_t table = a.t.page_off[a.t.V];
+  return (h.magic == kMagic) & (h.n_seq == a.n_seq) & (h.n_tokens == a.n_tokens) &
+         (h.V == a.t.V) & (h.table == table) & (h.G == a.pl.G) & (h.Hkv == a.pl.Hkv) &
+         (h.page_size == a.pl.P);
 }
 
 template <class T, int D>
