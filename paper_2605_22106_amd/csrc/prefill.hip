@@ -308,9 +308,70 @@ __device__ void merge_chains(const int32_t *n_kept, const O *page_off, const int
   }
 }
 
-// Cuts long tiles into parts and lists all parts, longest first; a workgroup of up to 16
-// waves.  Parts are in proportion to a tile's keys, rounded down: all parts together are no
-// more than `target` and the uncut tiles, so that they run at once.
+// Long tiles are cut into parts, and all parts listed, longest first.  Parts are in
+// proportion to a tile's keys, rounded down: all parts together are no more than `target`
+// and the uncut tiles, so that they run at once.
+struct Cut {
+  double per;            // parts per sub-page
+  int min_part;
+  __device__ Cut(int target, int64_t total, int least)
+      : per(total > 0 ? (double)target / (double)total : 0.0), min_part(least) {}
+  __device__ int parts(int s) const { return max(1, min((int)(s * per), s / min_part)); }
+  __device__ static int length(int s, int np) { return (s + np - 1) / np; }
+};
+
+// The np parts of tile k, from unit u and partial part0 on, by a wave.
+__device__ void list_parts(const PlanPtrs &p, int k, const Tile &tl, int np, int u, int part0) {
+  const int len = tl.n_sub / np, more = tl.n_sub % np;     // the first `more` have one more
+  for (int x = lane_id(); x < np; x += kWave)
+    if (u + x < p.units_cap)
+      p.units[u + x] = Unit{tl.t0, tl.nt, tl.n_ent, part0 + x, len * x + min(x, more),
+                            len * (x + 1) + min(x + 1, more), entry_base(k, tl.e0)};
+}
+
+__device__ void write_counts(const PlanPtrs &p, int units, int split, int target,
+                             int32_t *status) {
+  p.head->n_units = units;
+  p.head->n_split = split;
+  if (units > p.units_cap || split > target) status_error(status, ARBOR_ECORRUPT);
+  else p.head->magic = kMagic;
+}
+
+// Up to 64 tiles: four waves, one to a SIMD, have them all in their lanes and find their
+// order alone, a tile at a time; wave w lists the parts of the tiles 4 x + w.  (One tile in
+// three parts takes 2.1 us less than below, which waits at eight barriers.)
+__device__ void list_few(const PlanPtrs &p, const Tile *tiles, int n, int target, int min_part,
+                         int32_t *status) {
+  const int lane = lane_id(), wave = threadIdx.x / kWave, waves = 4;
+  if (wave >= waves) return;
+  Tile tl{};
+  if (lane < n) tl = tiles[lane];
+  const Cut cut(target, wave_sum((int64_t)tl.n_sub), min_part);
+  const int np = lane < n ? cut.parts(tl.n_sub) : 0;
+  const int len = np ? Cut::length(tl.n_sub, np) : 0;
+  const int many = np > 1 ? np : 0, part0 = wave_inclusive_scan(many) - many;
+  const uint64_t split = ballot(np > 1);
+  int u0 = 0, units = 0;
+  for (int j = 0; j < n; ++j) {
+    const int l = lane_value(len, j), m = lane_value(np, j);
+    u0 += l > len || (l == len && j < lane) ? m : 0;
+    units += m;
+  }
+  if (wave == 0) {
+    if (np > 1) {
+      const int x = popc(split & ((1ull << lane) - 1));
+      if (x < target) p.split[x] = int4{tl.t0, tl.nt, part0, np};
+    } else if (np == 1 && u0 < p.units_cap) {
+      p.units[u0] = Unit{tl.t0, tl.nt, tl.n_ent, -1, 0, tl.n_sub, entry_base(lane, tl.e0)};
+    }
+    if (lane == 0) write_counts(p, units, popc(split), target, status);
+  }
+  for (int j = wave; j < n; j += waves)
+    if (split >> j & 1) list_parts(p, j, tiles[j], lane_value(np, j), lane_value(u0, j),
+                                   lane_value(part0, j));
+}
+
+// Any number of tiles; a workgroup of up to 16 waves.
 __device__ void list_units(const PlanPtrs &p, const Tile *tiles, int n, int target, int min_part,
                            int32_t *status) {
   constexpr int NB = 256;
@@ -327,14 +388,12 @@ __device__ void list_units(const PlanPtrs &p, const Tile *tiles, int n, int targ
   for (int b = tid; b <= NB; b += nt) bucket[b] = 0;
   if (tid == 0) longest = 1;
   __syncthreads();
-  const double per = total > 0 ? (double)target / (double)total : 0.0;
-  auto share = [&](int s) { return max(1, min((int)(s * per), s / min_part)); };
-  auto length = [](int s, int np) { return (s + np - 1) / np; };
+  const Cut cut(target, total, min_part);
   int64_t v[2] = {0, 0}, ex[2], tot[2];        // parts of cut tiles, cut tiles
   int far = 0;
   for (int k = own; k < n; k += nt) {
-    const int s = k == own ? first.n_sub : tiles[k].n_sub, np = share(s);
-    far = max(far, length(s, np));
+    const int s = k == own ? first.n_sub : tiles[k].n_sub, np = cut.parts(s);
+    far = max(far, Cut::length(s, np));
     v[0] += np > 1 ? np : 0;
     v[1] += np > 1;
   }
@@ -343,8 +402,8 @@ __device__ void list_units(const PlanPtrs &p, const Tile *tiles, int n, int targ
   const float scale = (float)(NB - 1) / (float)longest;
   auto bucket_of = [&](int len) { return NB - 1 - min(NB - 1, (int)((float)len * scale)); };
   for (int k = own; k < n; k += nt) {
-    const int s = k == own ? first.n_sub : tiles[k].n_sub, np = share(s);
-    atomicAdd(&bucket[bucket_of(length(s, np))], np);
+    const int s = k == own ? first.n_sub : tiles[k].n_sub, np = cut.parts(s);
+    atomicAdd(&bucket[bucket_of(Cut::length(s, np))], np);
   }
   __syncthreads();
   if (tid < kWave) {
@@ -365,8 +424,8 @@ __device__ void list_units(const PlanPtrs &p, const Tile *tiles, int n, int targ
     int np = 0, u0 = 0, part0 = 0;
     if (k < n) {
       tl = k == own ? first : tiles[k];
-      np = share(tl.n_sub);
-      u0 = atomicAdd(&bucket[bucket_of(length(tl.n_sub, np))], np);
+      np = cut.parts(tl.n_sub);
+      u0 = atomicAdd(&bucket[bucket_of(Cut::length(tl.n_sub, np))], np);
       part0 = (int)ex[0];
       if (np > 1) {
         if (ex[1] < target) p.split[ex[1]] = int4{tl.t0, tl.nt, part0, np};
@@ -376,25 +435,13 @@ __device__ void list_units(const PlanPtrs &p, const Tile *tiles, int n, int targ
         p.units[u0] = Unit{tl.t0, tl.nt, tl.n_ent, -1, 0, tl.n_sub, entry_base(k, tl.e0)};
       }
     }
-    for (uint64_t cut = ballot(np > 1); cut; cut &= cut - 1) {      // a wave lists the parts
-      const int j = __builtin_ctzll(cut);
-      const int m = lane_value(np, j), u = lane_value(u0, j), s = lane_value(tl.n_sub, j);
-      const int len = s / m, more = s % m;           // the first `more` parts have one more
-      const Unit base{lane_value(tl.t0, j), lane_value(tl.nt, j), lane_value(tl.n_ent, j),
-                      lane_value(part0, j), 0, 0, entry_base(k0 + j * waves, lane_value(tl.e0, j))};
-      for (int x = lane; x < m; x += kWave)
-        if (u + x < p.units_cap)
-          p.units[u + x] = Unit{base.t0, base.nt, base.n_ent, base.part + x,
-                                len * x + min(x, more), len * (x + 1) + min(x + 1, more),
-                                base.ent};
+    for (uint64_t m = ballot(np > 1); m; m &= m - 1) {      // a wave lists the parts
+      const int j = __builtin_ctzll(m);
+      list_parts(p, k0 + j * waves, tiles[k0 + j * waves], lane_value(np, j), lane_value(u0, j),
+                 lane_value(part0, j));
     }
   }
-  if (tid == 0) {
-    p.head->n_units = units;
-    p.head->n_split = (int)tot[1];
-    if (units > p.units_cap || tot[1] > target) status_error(status, ARBOR_ECORRUPT);
-    else p.head->magic = kMagic;
-  }
+  if (tid == 0) write_counts(p, units, (int)tot[1], target, status);
 }
 
 // The whole plan of a call with few blocks and tiles, in one launch: a wave walks all
@@ -404,7 +451,8 @@ constexpr int kSmallTiles = 130, kSmallV = 4096;
 __global__ __launch_bounds__(1024) void plan_small(Tree t, int G, int Hkv, int P,
                                                    const int32_t *__restrict__ nodes, int n_seq,
                                                    const int32_t *__restrict__ cu, int n_tokens,
-                                                   PlanPtrs p, int target, int min_part, int32_t *status) {
+                                                   PlanPtrs p, int target, int min_part,
+                                                   int32_t *status) {
   __shared__ int32_t depth[kWave], sh_cu[kWave + 1];
   __shared__ int32_t sh_parent[kSmallV], sh_kept[kSmallV], sh_page_off[kSmallV];
   __shared__ uint16_t chain[MAXD * kCol];
@@ -442,7 +490,8 @@ __global__ __launch_bounds__(1024) void plan_small(Tree t, int G, int Hkv, int P
   }
   if (threadIdx.x == 0) write_header(p, t, G, Hkv, P, n_seq, n_tokens, n_tiles);
   __syncthreads();
-  list_units(p, tiles, n_tiles, target, min_part, status);
+  if (n_tiles <= kWave) list_few(p, tiles, n_tiles, target, min_part, status);
+  else list_units(p, tiles, n_tiles, target, min_part, status);
 }
 
 // The same in three launches: tiles, a wave for each tile's chains, parts.
