@@ -460,8 +460,9 @@ def _stream_of(stream, device: int) -> int:
 def _descriptors(kv: KVState):
     """(device, geometry, tree, pool, n_full) of kv's tensors for a call; built again when a
     field of kv has been set, or one of its tensors been moved or resized in place."""
-    now = (kv.parent.numel(), kv.k.numel(), kv.parent.data_ptr(), kv.n_full.data_ptr(), kv.tok_off.data_ptr(),
-           kv.page_off.data_ptr(), kv.n_kept.data_ptr(), kv.page_table.data_ptr(),
+    now = (kv.parent.numel(), kv.k.numel(), kv.parent.data_ptr(), kv.n_full.data_ptr(),
+           kv.tok_off.data_ptr(), kv.page_off.data_ptr(), kv.n_kept.data_ptr(),
+           kv.page_table.data_ptr(),
            kv.k.data_ptr(), kv.v.data_ptr(), kv.slot_pos.data_ptr(), kv.free_stack.data_ptr(),
            kv.free_top.data_ptr())
     d = kv.__dict__.get("_built")
