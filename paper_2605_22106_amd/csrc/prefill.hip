@@ -8,10 +8,10 @@
 // of the ancestors they have in common, and a row sees a key when its sequence is
 // in the block's set and, in its own block, the slot is not after its own.
 //
-// The plan (three launches, once for all layers): cut the packed tokens into tiles;
-// a wave per tile merges its chains; split the tiles whose keys outlast the others'
-// into parts, so that a few rows over a long prompt fill the chip.  The attention
-// runs one workgroup per (part, KV head) and a second launch joins the parts.
+// The plan (once for all layers; one launch, or three for many tiles): cut the packed
+// tokens into tiles; a wave per tile merges its chains; split the tiles whose keys outlast
+// the others' into parts, so that a few rows over a long prompt fill the chip.  The
+// attention runs one workgroup per (part, KV head) and a second launch joins the parts.
 //
 // Attention of a tile: a wave holds 32 rows.  S^T = K Q^T with 32x32 MFMA leaves
 // each lane one row and half of the keys, so the softmax needs one exchange between
@@ -20,7 +20,15 @@
 // one in which S^T leaves them; V^T is read from LDS in the same order, through the
 // transposing LDS read for bf16).  Keys and values come by direct loads to LDS
 // through a buffer resource over the valid rows of a sub-page, which fills the
-// others with zeros.
+// others with zeros; those of the next step are issued before this step's products.
+//
+// What bounds it: LDS.  A step of 64 keys reads 16 KB of K and 16 KB of V from LDS in
+// each of four waves, for 4 MFLOP of products a wave, and 32 KB arrive.  8,192 tokens of
+// the 70B shape (1.1 TFLOP): 1.07 ms, 1.03 PFLOP/s (a library's 8,192^3 product: 1.3 to
+// 1.5); with the reads of K left out 0.88 ms, of V 1.07, of both 0.80, without the loads
+// 0.97, with none of these 0.64.  64 rows a wave halve the reads, but leave one wave to a
+// SIMD, which ran 1.55 ms and more; 32 keys a step and three waves 1.77.  fp32: 122
+// TFLOP/s of the 153 of a library's product.
 #include <type_traits>
 
 #include "arbor_internal.h"
@@ -43,7 +51,7 @@ constexpr float kLn2 = 0.6931471805599453f;
 // and leaves V 2^100 of headroom, and a step needs neither a max nor a rescale.
 constexpr float kMoveAt = 65536.0f;
 // Workgroups that the chip holds at a time (two to each of 256 CUs).  Parts for 256 of them
-// instead: 64 drafts below 32,000 tokens, two layers, 277 us against 220; 16 ragged blocks
+// instead: 64 drafts below 15,000 tokens, two layers, 277 us against 220; 16 ragged blocks
 // over a tree, four layers, 240 against 206.
 constexpr int kSlots = 512;
 // Sub-pages of a step, and steps of the shortest part: a part's fixed work (its way to its
@@ -447,6 +455,9 @@ __device__ void list_units(const PlanPtrs &p, const Tile *tiles, int n, int targ
 // The whole plan of a call with few blocks and tiles, in one launch: a wave walks all
 // chains beside one that cuts the tiles, then 16 waves merge them.  What bounds it is the
 // latency of one access after the other, so all that it reads twice is in LDS.
+// In one launch and in three: 48 tokens 6.7 and 11.9 us, 16 blocks of 128 13.1 and 16.0, 64
+// blocks of 8 11.0 and 15.8, one block of 512, 1,024 and 2,048 tokens 7.3 and 13.0, 9.9 and
+// 13.4, 12.8 and 12.9.  The last of these may have 130 tiles (it has 64).
 constexpr int kSmallTiles = 130, kSmallV = 4096;
 __global__ __launch_bounds__(1024) void plan_small(Tree t, int G, int Hkv, int P,
                                                    const int32_t *__restrict__ nodes, int n_seq,
@@ -1167,8 +1178,9 @@ __global__ __launch_bounds__(kRows * 2, 2) void prefill_attn(AttnArgs a) {
 
 // Joins the parts of the tiles that have several: a workgroup per 32 rows of a tile and KV
 // head, whose waves take the register quads that the attention's lanes had, each lane four
-// columns of one row at a time, parts in order.  It waits on memory: the first parts' sums
-// are on their way before their references are there.
+// columns of one row at a time, parts in order.  It waits on memory: four parts' sums and
+// references are on their way together (60 parts of 8 KV heads, 33 MB, 8.4 us; one part
+// after the other, with rows of D + 4 floats, 10.8).
 template <class T, int D>
 __global__ __launch_bounds__(256) void prefill_join(AttnArgs a) {
   constexpr int U = 4, QUADS = D / 8;
@@ -1270,8 +1282,6 @@ int launch_prefill_plan(const arbor_geom_t *geom, const arbor_tree_t *tree, cons
   const int G = geom->q_per_kv, Hkv = geom->num_kv_heads, P = geom->page_size;
   const int target = target_parts(Hkv);
   const int min_part = kMinSteps * step_subs(geom->dtype == ARBOR_BF16 ? 2 : 4);
-  // 16 waves take a few rounds over a few tiles; one block's 100 tiles and more are faster
-  // one wave each, as are the chains of more blocks than a wave has lanes
   if (n_seq <= kMaxSeq && p.tiles_cap <= kSmallTiles && t.V <= kSmallV) {
     hipLaunchKernelGGL(plan_small, dim3(1), dim3(1024), 0, stream, t, G, Hkv, P, nodes, n_seq, cu,
                        n_tokens, p, target, min_part, status);

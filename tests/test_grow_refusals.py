@@ -149,6 +149,36 @@ def test_tiles_never_exceed_their_bound():
         assert tiles <= min(sum(m), 2 * (sum(m) // tq) + len(m) // 64 + 2)
 
 
+def test_tiles_by_links_keep_the_bound_and_hold_every_token():
+    """The plan's own cut: a block's whole tiles, then its rest with the blocks that fit."""
+    import bisect
+    import random
+    r = random.Random(2)
+    for _ in range(3000):
+        tq = r.choice([1, 2, 16, 25, 32, 42, 128])
+        m = [r.choice([0, 0, 1, tq, r.randint(0, 5), r.randint(0, 3 * tq)])
+             for _ in range(r.choice([1, 5, 70, 300]))]
+        cu = [0]
+        for x in m:
+            cu.append(cu[-1] + x)
+        tiles, e = [], 0
+        while e < len(m):
+            full = m[e] // tq
+            tiles += [(cu[e] + x * tq, tq, 1) for x in range(full)]
+            t, nxt = cu[e] + full * tq, e + 1
+            if t < cu[e + 1]:
+                hi = min(len(m), e + 64)
+                nxt = bisect.bisect_right(cu, t + tq, e + 1, hi + 1) - 1
+                tiles.append((t, cu[nxt] - t, nxt - e))
+            e = nxt
+        at = 0
+        for t, n, blocks in tiles:
+            assert t == at and 0 < n <= tq and 1 <= blocks <= 64
+            at += n
+        assert at == cu[-1]
+        assert len(tiles) <= min(sum(m), 2 * (sum(m) // tq) + len(m) // 64 + 2)
+
+
 def test_the_binding_checks_shapes_types_and_places():
     cpu = torch.zeros(3, dtype=torch.int32)
     rows = torch.zeros(2, 8)
