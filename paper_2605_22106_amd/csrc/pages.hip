@@ -21,6 +21,7 @@ namespace arbor {
 namespace {
 
 constexpr int kPlanThreads = 1024;
+constexpr int kTreeLds = 4096;          // blocks of a tree that a plan keeps in LDS
 
 // What the plan leaves for the second launch, one entry per listed block.
 struct Grow {
@@ -50,7 +51,6 @@ __device__ __forceinline__ int last_at_most(const T *first, int n, T x) {
 
 // Tokens that the block x gets in this call (0 unless it is listed).
 __device__ __forceinline__ int listed_tokens(const int32_t *nodes, const int32_t *cu, int n, int x) {
-  if (x < nodes[0]) return 0;          // a tree's newest blocks: no ancestor is listed
   const int e = last_at_most(nodes, n, x);
   return nodes[e] == x ? cu[e + 1] - cu[e] : 0;
 }
@@ -90,13 +90,22 @@ __device__ void extend_rows(const Tree &t, const Pool &pl, const int32_t *__rest
   }
 }
 
-// Latency: the chain walk is a dependent load per level, then two barriers (7.1 us for 48
-// blocks and 288 tokens, 7.9 for 16 blocks four levels down and 496 tokens).
+// Latency: checks 1.3 us, a vote 0.5, walks 1.1, scan 0.8, rows 1.5 (6.6 us for 48 blocks and
+// 288 tokens, 7.4 for 16 blocks four levels down and 496 tokens; walks in memory, a dependent
+// load a level: 7.9).
 __global__ __launch_bounds__(kPlanThreads) void extend_plan(
     Tree t, Pool pl, int32_t *n_full, const int32_t *__restrict__ nodes, int n_seq,
     const int32_t *__restrict__ cu, int n_tokens, Grow g, int64_t *__restrict__ slots,
     int32_t *__restrict__ positions, int64_t *__restrict__ tokens, int rows_too, int32_t *status) {
   __shared__ int64_t sm[17];
+  // the tree itself, where it is small, so that a walk's steps do not wait for memory
+  __shared__ int32_t sh_parent[kTreeLds], sh_full[kTreeLds];
+  const bool near = t.V <= kTreeLds;
+  if (near)
+    for (int i = threadIdx.x; i < t.V; i += blockDim.x) {
+      sh_parent[i] = t.parent[i];
+      sh_full[i] = t.n_full[i];
+    }
   if (status_failed(status)) {
     if (threadIdx.x == 0) g.meta[0] = 0;
     return;
@@ -106,6 +115,7 @@ __global__ __launch_bounds__(kPlanThreads) void extend_plan(
   const int r0 = min(n_seq, (int)threadIdx.x * per), r1 = min(n_seq, r0 + per);
   int err = 0;
   int64_t need = 0;
+  const int top = *pl.free_top, oldest = n_seq > 0 ? nodes[0] : 0;
   if (threadIdx.x == 0 && (cu[0] != 0 || cu[n_seq] > n_tokens || cu[n_seq] < 0)) err = ARBOR_EINVAL;
   for (int e = r0; e < r1; ++e) {
     const int i = nodes[e], m = cu[e + 1] - cu[e];
@@ -135,7 +145,7 @@ __global__ __launch_bounds__(kPlanThreads) void extend_plan(
     int64_t start = 0;
     int depth = 0;
     for (int x = nodes[e];;) {
-      const int up = t.parent[x];
+      const int up = near ? sh_parent[x] : t.parent[x];
       if (up < 0) break;
       if (up >= x) {
         err = ARBOR_EINVAL;
@@ -146,13 +156,13 @@ __global__ __launch_bounds__(kPlanThreads) void extend_plan(
         break;
       }
       x = up;
-      start += t.n_full[x] + listed_tokens(nodes, cu, n_seq, x);
+      start += (near ? sh_full[x] : t.n_full[x]) +
+               (x < oldest ? 0 : listed_tokens(nodes, cu, n_seq, x));
     }
     g.start[e] = (int32_t)start;
   }
   int64_t total;
   const int64_t base = block_exclusive_scan(need, sm, &total);
-  const int top = *pl.free_top;
   if (total > top) err = err ? err : ARBOR_ENOPAGES;
   if (__syncthreads_or(err)) {
     if (err) status_error(status, err);
@@ -221,6 +231,7 @@ __global__ __launch_bounds__(kPlanThreads) void truncate_plan(
   const int r0 = min(n_nodes, (int)threadIdx.x * per), r1 = min(n_nodes, r0 + per);
   int err = 0;
   int64_t touched = 0, freed = 0;
+  const int top = *pl.free_top;
   for (int e = r0; e < r1; ++e) {
     const int i = nodes[e];
     if (i < 0 || i >= t.V || (e > 0 && nodes[e - 1] >= i) || keep[e] < 0) {
@@ -242,7 +253,6 @@ __global__ __launch_bounds__(kPlanThreads) void truncate_plan(
   const int64_t v[2] = {touched, freed};
   int64_t ex[2], tot[2];
   block_exclusive_scan_n<2>(v, ex, tot, sm);
-  const int top = *pl.free_top;
   if (!err && (top < 0 || top + tot[1] > pl.num_pages)) err = ARBOR_ECORRUPT;
   if (__syncthreads_or(err)) {
     if (err) status_error(status, err);
@@ -267,19 +277,24 @@ __global__ __launch_bounds__(kPlanThreads) void truncate_plan(
   }
 }
 
-// (The plan takes 4.2 to 5.2 us, this launch 3.9 to 5.4, mostly their start and the latency of
+// (The plan takes 3.5 to 4.7 us, this launch 3.5 to 4.4, mostly their start and the latency of
 // five loads; the host does not know how many pages there are, so it is always made.)
 // 16 lanes a page: the slots from the first vacated one on, and, where the page is
 // freed, its table entry and its place on the stack.
 __global__ __launch_bounds__(256) void truncate_clear(Tree t, Pool pl,
                                                       const int32_t *__restrict__ nodes,
                                                       int n_nodes, Grow g, int32_t *status) {
+  __shared__ int32_t sh_first[1024];
+  const bool few = n_nodes <= 1024;
+  if (few)
+    for (int e = threadIdx.x; e < n_nodes; e += 256) sh_first[e] = g.first[e];
   if (status_failed(status) || !g.meta[0]) return;
   const int P = pl.P, lane = threadIdx.x % 16;
   const int top = g.meta[1], total = g.meta[2], freed = g.meta[3];
+  __syncthreads();
   for (int x = (blockIdx.x * blockDim.x + threadIdx.x) / 16; x < total;
        x += gridDim.x * blockDim.x / 16) {
-    const int e = last_at_most(g.first, n_nodes, x);
+    const int e = few ? last_at_most(sh_first, n_nodes, x) : last_at_most(g.first, n_nodes, x);
     const int i = nodes[e], left = g.start[e];
     const int q = left / P + x - g.first[e];
     const int64_t at = t.page_off[i] + q;
@@ -309,6 +324,7 @@ __global__ __launch_bounds__(kPlanThreads) void fork_plan(Tree t, Pool pl, int32
   const int r0 = min(n_forks, (int)threadIdx.x * per), r1 = min(n_forks, r0 + per);
   int err = 0;
   int64_t need = 0;
+  const int top = *pl.free_top;
   for (int e = r0; e < r1; ++e) {
     const int a = src[e], b = dst[e];
     if (a < 0 || a >= t.V || b < 0 || b >= t.V || (e > 0 && dst[e - 1] >= b)) {
@@ -329,7 +345,6 @@ __global__ __launch_bounds__(kPlanThreads) void fork_plan(Tree t, Pool pl, int32
   }
   int64_t total;
   const int64_t base = block_exclusive_scan(need, sm, &total);
-  const int top = *pl.free_top;
   if (!err && total > top) err = ARBOR_ENOPAGES;
   // (after this barrier every source has been read, one that is a destination too
   // as it was)
@@ -434,7 +449,10 @@ int launch_extend(const arbor_geom_t *geom, arbor_tree_t *tree, arbor_pool_t *po
   if (!carve(g, n_seq, workspace, workspace_bytes)) return ARBOR_EWORKSPACE;
   // up to 4,096 tokens the plan's workgroup writes their rows itself
   const int rows_too = n_tokens <= 4 * kPlanThreads;
-  hipLaunchKernelGGL(extend_plan, dim3(1), dim3(kPlanThreads), 0, stream, t, pl, n_full, nodes,
+  // few waves meet at a barrier sooner (48 blocks, 288 tokens: 6.6 us, 7.1 with 1,024
+  // threads), but a thread that has two tokens waits twice (496: 8.0, 7.4)
+  const int threads = n_seq <= 256 && n_tokens <= 320 ? 256 : kPlanThreads;
+  hipLaunchKernelGGL(extend_plan, dim3(1), dim3(threads), 0, stream, t, pl, n_full, nodes,
                      n_seq, cu, n_tokens, g, slots, positions, tokens, rows_too, status);
   if (!rows_too) {
     const int blocks = (n_tokens + 255) / 256 < 2048 ? (n_tokens + 255) / 256 : 2048;
@@ -452,7 +470,7 @@ int launch_truncate(const arbor_geom_t *geom, arbor_tree_t *tree, arbor_pool_t *
   if (n_nodes == 0) return ARBOR_OK;
   Grow g;
   if (!carve(g, n_nodes, workspace, workspace_bytes)) return ARBOR_EWORKSPACE;
-  hipLaunchKernelGGL(truncate_plan, dim3(1), dim3(kPlanThreads), 0, stream, t, pl, n_full, nodes,
+  hipLaunchKernelGGL(truncate_plan, dim3(1), dim3(n_nodes <= 256 ? 256 : kPlanThreads), 0, stream, t, pl, n_full, nodes,
                      keep, n_nodes, g, status);
   hipLaunchKernelGGL(truncate_clear, dim3(128), dim3(256), 0, stream, t, pl, nodes, n_nodes, g,
                      status);
@@ -468,7 +486,7 @@ int launch_fork(const arbor_geom_t *geom, arbor_tree_t *tree, arbor_pool_t *pool
   if (n_forks == 0) return ARBOR_OK;
   Grow g;
   if (!carve(g, n_forks, workspace, workspace_bytes)) return ARBOR_EWORKSPACE;
-  hipLaunchKernelGGL(fork_plan, dim3(1), dim3(kPlanThreads), 0, stream, t, pl, n_full, src, dst,
+  hipLaunchKernelGGL(fork_plan, dim3(1), dim3(n_forks <= 256 ? 256 : kPlanThreads), 0, stream, t, pl, n_full, src, dst,
                      n_forks, g, rows_seen, status);
   const int copies = 2048;
   const int marks = A ? (n_forks < 256 ? n_forks : 256) : 0;

@@ -341,3 +341,59 @@ def test_timing_of_the_attention():
                                        timing=L.timing(L.KERNEL_PREFILL_ATTN, a, b)))
     assert same(step.results(), want)
     assert 0.0 < a.elapsed_time(b) < 1000.0
+
+
+def test_blocks_to_come_are_scored():
+    """Score over a tree with spare capacity and blocks that hold nothing yet, against the
+    oracle."""
+    st = small_state(seed=7)
+    for x in ("k", "v"):                           # rows that hold nothing are not read
+        assert bool(torch.isnan(st[x]).any())
+    kv, ost, V, N, W = to_gpu(st), oracle_state(st), 9, st["num_tokens"], 8
+    Hq, gen = 8, torch.Generator().manual_seed(2)
+    obs, sl = [3, 4, 5], [0, 1]
+    qw = torch.randn((3, 2, Hq, W, 128), generator=gen).bfloat16()
+    vs, us = torch.rand(V, generator=gen), torch.rand(V, generator=gen)
+    A, rows = torch.zeros(N, device="cuda"), torch.zeros(V, dtype=torch.int64, device="cuda")
+    a, s, stt = torch.empty(V, device="cuda"), torch.empty(V, device="cuda"), status()
+    check_rc(L.arbor_score(kv, i32(obs), qw.cuda(), W, sl, vs.cuda(), us.cuda(), A, rows, a, s,
+                           PARAMS, stt, workspace(kv, max_observers=3, window=W, n_slice=2)))
+    Ao, ro, ao, so = O.score(ost, obs, np_float(qw), W, sl, 4, vs.numpy(), us.numpy(),
+                             np.zeros(N, np.float32), np.zeros(V, np.int64), theta=PARAMS["theta"],
+                             self_window=0)
+    assert int(stt) == 0 and np.array_equal(rows.cpu().numpy(), ro)
+    full = st["n_full"].numpy() > 0
+    for got, want in ((A.cpu().numpy(), Ao), (a.cpu().numpy()[full], ao[full]),
+                      (s.cpu().numpy()[full], so[full])):
+        assert np.all(np.abs(got - want) <= 1e-4 * np.abs(want) + 1e-30)
+    assert bool(torch.isfinite(a).all()) and bool(torch.isfinite(s).all())
+
+
+def test_rows_beyond_four_gib():
+    """Append, attention and forks where the pool's byte offsets pass 32 bits: the same bits
+    as in a small pool."""
+    st = grow_state([-1, 0, 0], [300, 40, 0], spare=300, kv_heads=8, q_per_kv=4, head_dim=128,
+                    dtype="bf16", layers=1, extra_pages=8)
+    small = to_gpu(st)
+    far, pages = 150_000, st["num_pages"]          # 32 KiB a page of K: 4.9 GB before these
+    st2 = dict(st, num_pages=far + pages)
+    for x in ("k", "v"):
+        st2[x] = torch.empty((1, 1, 8, 16, 128), dtype=torch.bfloat16)
+    for x in ("page_table", "free_stack"):
+        st2[x] = torch.where(st[x] >= 0, st[x] + far, st[x])
+    st2["slot_pos"] = torch.cat((torch.full((far, 16), -1, dtype=torch.int32), st["slot_pos"]))
+    st2["free_stack"] = torch.cat((st2["free_stack"], torch.full((far,), -1, dtype=torch.int32)))
+    big = to_gpu(st2)
+    for x in ("k", "v"):
+        y = torch.empty((1, far + pages, 8, 16, 128), dtype=torch.bfloat16, device="cuda")
+        y[:, far:] = getattr(small, x)
+        setattr(big, x, y)
+    a, b = (Step(kv, [0, 1], [70, 33]) for kv in (small, big))
+    for s in (a, b):
+        s()
+        check_rc(L.arbor_fork(s.kv, i32([1]), i32([2]), s.status, s.ws2))
+    assert int(a.status) == int(b.status) == 0
+    assert torch.equal(a.q, b.q) and torch.equal(a.out, b.out) and torch.equal(a.lse, b.lse)
+    assert torch.equal(a.slots + 16 * far, b.slots)
+    for x, y in ((small.k, big.k), (small.v, big.v)):
+        assert torch.equal(x.view(torch.int16), y[:, far:].view(torch.int16))
