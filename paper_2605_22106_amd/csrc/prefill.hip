@@ -115,6 +115,14 @@ __host__ __device__ inline int target_parts(int Hkv) {
   return t > 0 ? t : 1;
 }
 
+// Whether the plan may cut a tile.  Of one block with twice as many tiles as the chip holds
+// for a KV head, none has more than about twice the average's keys, so none would be: the
+// call goes without the second launch (6 us a layer of 164, 4,096 tokens of the 8B shape).
+inline bool may_split(const arbor_geom_t *g, int n_seq, int n_tokens) {
+  return n_seq > 1 ||
+         n_tokens / tokens_per_tile(g->q_per_kv) < 2 * target_parts(g->num_kv_heads);
+}
+
 PlanPtrs carve_plan(const arbor_geom_t *g, int n_seq, int n_tokens, void *plan, size_t bytes,
                     size_t *need) {
   PlanPtrs p{};
@@ -1281,7 +1289,8 @@ int launch_prefill_plan(const arbor_geom_t *geom, const arbor_tree_t *tree, cons
   const Tree t = make_tree(tree);
   const int G = geom->q_per_kv, Hkv = geom->num_kv_heads, P = geom->page_size;
   const int target = target_parts(Hkv);
-  const int min_part = kMinSteps * step_subs(geom->dtype == ARBOR_BF16 ? 2 : 4);
+  const int min_part = may_split(geom, n_seq, n_tokens)
+                           ? kMinSteps * step_subs(geom->dtype == ARBOR_BF16 ? 2 : 4) : INT32_MAX;
   if (n_seq <= kMaxSeq && p.tiles_cap <= kSmallTiles && t.V <= kSmallV) {
     hipLaunchKernelGGL(plan_small, dim3(1), dim3(1024), 0, stream, t, G, Hkv, P, nodes, n_seq, cu,
                        n_tokens, p, target, min_part, status);
@@ -1321,7 +1330,8 @@ int launch_prefill(const arbor_geom_t *geom, const arbor_tree_t *tree, const arb
   const int target = target_parts(geom->num_kv_heads);
   const int64_t units = a.p.units_cap * geom->num_kv_heads;
   // tiles of two parts or more
-  const int64_t split = a.p.tiles_cap < target / 2 ? a.p.tiles_cap : target / 2;
+  const int64_t split = !may_split(geom, n_seq, n_tokens) ? 0
+                        : a.p.tiles_cap < target / 2 ? a.p.tiles_cap : target / 2;
   if (units > INT32_MAX) return ARBOR_EUNSUPPORTED;
 #define ARBOR_PREFILL_LAUNCH(T, D)                                                             \
   do {                                                                                         \

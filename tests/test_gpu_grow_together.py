@@ -310,6 +310,27 @@ def test_a_plan_of_another_tree():
     assert int(pf.status) == L.EINVAL and bool((out == 7.0).all())
 
 
+@pytest.mark.parametrize("had,T,G", [(0, 1100, 8), (777, 1024, 8), (300, 67, 128), (0, 8200, 1)])
+def test_one_block_of_many_tiles(had, T, G):
+    """Twice as many tiles as the chip holds for a KV head: a call without parts."""
+    heads = 16 if G < 128 else 64
+    st = grow_state([-1, 0], [had, T], spare=0, kv_heads=heads, q_per_kv=G, head_dim=64,
+                    dtype="bf16", seed=6, layers=1)
+    kv = to_gpu(st)
+    pf, q = Prefill(kv, [1], [T]), queries(kv, T)
+    pf.ws.fill_(255)                               # (NaN, if parts were read)
+    got = pf(q)
+    assert int(pf.status) == 0
+    dev = {k: v.cuda() if torch.is_tensor(v) else v for k, v in st.items()}
+    if T * G < 10000:
+        check(got, reference(dev, [-1, 0], [1], [T], 0, q, G), "bf16", 64)
+        return
+    # the last tokens alone are the reference's; more of them would not fit its matrices
+    last = 40
+    want = reference(dev, [-1, 0], [1], [last], 0, q[T - last:], G)
+    check(tuple(x[T - last:] for x in got), want, "bf16", 64)
+
+
 @pytest.mark.parametrize("T", [8191, 8192, 8700])
 @pytest.mark.parametrize("inter", [False, True])
 def test_append_of_many_tokens(T, inter):
