@@ -7,8 +7,7 @@
 // through LDS; then every group of D / 8 lanes takes one head, eight elements a lane.
 // The sum of squares crosses the lanes by DPP; nothing but the angles goes through LDS,
 // and each element is read and written once: HBM-bound.  The norm's factor comes last: a
-// bf16 element times its weight is exact in fp32, and the fewer roundings before the last
-// one, the fewer elements fall on its other side.
+// bf16 element times its weight is exact in fp32.
 //
 // Where a pair of the rotation lies in one lane's 16 bytes (neighbours) or in those of the
 // lane half a head further on (halves of a whole head), a lane takes eight elements in a
@@ -41,8 +40,8 @@ struct Piece<float> {
 };
 
 // sum over the LPR lanes of a row's group, in each of them
-template <int LPR>
-__device__ __forceinline__ float row_sum(float v) {
+template <int LPR, class F>
+__device__ __forceinline__ F row_sum(F v) {
   v += dpp_move<dpp::kQuadXor1>(v);
   v += dpp_move<dpp::kQuadXor2>(v);
   v += dpp_move<dpp::kRowHalfMirror>(v);
@@ -59,7 +58,8 @@ __device__ __forceinline__ uint32_t other_half(uint32_t v) {
 
 // sin and cos of 2 pi x by their Taylor series, after x is brought to an eighth of a turn
 // on either side of a quarter: the first terms left out are 5e-17 and 2e-18.
-__device__ __forceinline__ void sin_cos_turns(double x, float *s, float *c) {
+template <class F>
+__device__ __forceinline__ void sin_cos_turns(double x, F *s, F *c) {
   x -= rint(x);                                 // (exact)
   const double k = rint(4.0 * x);
   const double r = (x - 0.25 * k) * 6.283185307179586476925, z = r * r;
@@ -71,11 +71,23 @@ __device__ __forceinline__ void sin_cos_turns(double x, float *s, float *c) {
   ps = fma(ps, z, 1.0 / 120.0), pc = fma(pc, z, -1.0 / 720.0);
   ps = fma(ps, z, -1.0 / 6.0), pc = fma(pc, z, 1.0 / 24.0);
   pc = fma(pc, z, -0.5);
-  const float sr = (float)fma(r * z, ps, r), cr = (float)fma(pc, z, 1.0);
+  const F sr = (F)fma(r * z, ps, r), cr = (F)fma(pc, z, 1.0);
   const int quarter = (int)k & 3;
-  const float u = quarter & 1 ? cr : sr, v = quarter & 1 ? sr : cr;
+  const F u = quarter & 1 ? cr : sr, v = quarter & 1 ? sr : cr;
   *s = quarter & 2 ? -u : u;
   *c = (quarter + 1) & 2 ? -v : v;
+}
+
+// A bf16 result is formed again in 64 bits where its fp32 value lies within so many last
+// places of the middle between two bf16: the roundings of the norm's factor (three), of
+// sine and cosine, and of two products, a sum and the result are less than that together.
+constexpr uint32_t kTie = 6;
+
+// 1 / sqrt(x) by the instruction, good to 2^-23 or so, and two steps of Newton's method
+__device__ __forceinline__ double inverse_root(double x) {
+  const double r = __builtin_amdgcn_rsq(x);
+  const double n = fma(0.5 * r, fma(-x * r, r, 1.0), r), m = fma(0.5 * n, fma(-x * n, n, 1.0), n);
+  return r > 0.0 && r < 1.0e300 ? m : r;        // (0 of an infinity, infinity of 0)
 }
 
 template <class T, int D>
@@ -216,21 +228,27 @@ __global__ __launch_bounds__(256) void append_rows(AppendArgs args) {
 }
 
 // The same with eight elements in a row a lane; see above.  A step's registers take the
-// next load as soon as they are read, and three in flight leave eight waves to a SIMD (six,
-// with four in flight: 87 us).  Each line is read once and written once, past the caches
-// (81 us with ordinary stores).  8,192 tokens of 64 + 8 + 8 heads of 128 bf16, 336 MB:
-// 74 us, 4.5 TB/s of the 5.1 of a large copy.
+// next load as soon as they are read; where a wave takes a token by itself two in flight,
+// with the sines read from LDS, leave eight waves to a SIMD (six: 87 us and more).  Each
+// line is read once and written once, past the caches (7 us more with ordinary stores).
+// 8,192 tokens of 64 + 8 + 8 heads of 128 bf16, 336 MB: 76 us, 4.4 TB/s of the 5.1 of a
+// large copy.
+//
+// A bf16 that fp32 rounds to the other side moves its key's logits by up to 2^-8 of a
+// product, so the few results that fp32 does not decide are formed again in 64 bits (2 us
+// of the 76; all of them in 64 bits: 94 us and more).
 template <class T, int D, bool HALVES, int BLOCK>
-__global__ __launch_bounds__(BLOCK, sizeof(T) == 2 ? 8 : 4) void append_whole(AppendArgs args) {
+__global__ __launch_bounds__(BLOCK, BLOCK == 64 && sizeof(T) == 2 ? 8 : 4) void append_whole(AppendArgs args) {
   constexpr int LPR = D / 8;                    // lanes of a head
   constexpr int RPS = BLOCK / LPR;              // heads a step
-  constexpr int UNROLL = 3;                     // steps whose loads are in flight together
+  constexpr int UNROLL = BLOCK == 64 ? 2 : 4;   // steps whose loads are in flight together
   constexpr int W = sizeof(T) * 2;              // words of eight elements
   struct Eight {
     T e[8];
   };
   typedef uint32_t words __attribute__((ext_vector_type(W), aligned(16)));
-  __shared__ __attribute__((aligned(16))) float sh_cos[D / 2], sh_sin[D / 2];
+  __shared__ __attribute__((aligned(16))) double sh_cos[D / 2], sh_sin[D / 2];
+  __shared__ __attribute__((aligned(16))) float near_cos[D / 2], near_sin[D / 2];
   const arbor_append_t &a = args.a;
   const Pool &pl = args.pl;
   const int64_t t = blockIdx.x;
@@ -266,20 +284,18 @@ __global__ __launch_bounds__(BLOCK, sizeof(T) == 2 ? 8 : 4) void append_whole(Ap
   if (rd > 0) {
     // in turns: pos f / (2 pi) in fp64 is off by 2^-53 relative, 1e-10 turns at position
     // 10^6
-    if (tid < half)
-      sin_cos_turns((double)pos * freq * 0.15915494309189535, &sh_sin[tid], &sh_cos[tid]);
+    if (tid < half) {
+      double s, c;
+      sin_cos_turns((double)pos * freq * 0.15915494309189535, &s, &c);
+      sh_sin[tid] = s, sh_cos[tid] = c;
+      near_sin[tid] = (float)s, near_cos[tid] = (float)c;
+    }
     __syncthreads();
   }
   // element e becomes own co + partner si
   const bool turns = 8 * q8 < rd;
-  float co[8], si[8];
-#pragma unroll
-  for (int e = 0; e < 8; ++e) {
-    const int pair = HALVES ? (8 * q8 + e) & (D / 2 - 1) : 4 * q8 + e / 2;
-    const bool first = HALVES ? 8 * q8 < half : e % 2 == 0;
-    co[e] = turns ? sh_cos[pair] : 1.0f;
-    si[e] = turns ? first ? -sh_sin[pair] : sh_sin[pair] : 0.0f;
-  }
+  auto pair = [&](int e) { return HALVES ? (8 * q8 + e) & (D / 2 - 1) : 4 * q8 + e / 2; };
+  auto first = [&](int e) { return HALVES ? 8 * q8 < half : e % 2 == 0; };
   const int64_t page = slot / pl.P, row = slot % pl.P;
   for (; h0 < heads; h0 += UNROLL * RPS) {
 #pragma unroll
@@ -320,8 +336,38 @@ __global__ __launch_bounds__(BLOCK, sizeof(T) == 2 ? 8 : 4) void append_whole(Ap
           }
         }
         Eight out;
+        uint32_t near = ~0u;
+        asm volatile("" ::: "memory");   // (the sines are read here, not kept in registers)
 #pragma unroll
-        for (int e = 0; e < 8; ++e) out.e[e] = (T)(r * (turns ? v[e] * co[e] + p[e] * si[e] : v[e]));
+        for (int e = 0; e < 8; ++e) {
+          const float s = near_sin[pair(e)];
+          const float f = r * (turns ? v[e] * near_cos[pair(e)] + p[e] * (first(e) ? -s : s) : v[e]);
+          out.e[e] = (T)f;
+          near = min(near, (__builtin_bit_cast(uint32_t, f) - (0x8000 - kTie)) & 0xffff);
+        }
+        if (sizeof(T) == 2 && __builtin_expect(ballot(near <= 2 * kTie) != 0, 0)) {
+          // (one step of eight; v and p are exact)
+          asm volatile("" ::: "memory");
+          double x = 1.0;
+          if (w) {
+            float ss = 0.0f;                         // (of exact squares)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) ss += (float)own.e[e] * (float)own.e[e];
+            x = inverse_root(row_sum<LPR>((double)ss) * (1.0 / D) + a.eps);
+          }
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            double y = v[e];
+            if (turns) {
+              const double s = sh_sin[pair(e)];
+              y = fma((double)p[e], first(e) ? -s : s, y * sh_cos[pair(e)]);
+            }
+            float f = (float)(y * x);
+            asm volatile("" : "+v"(f));
+            out.e[e] = (T)f;
+            __builtin_amdgcn_sched_barrier(0);       // (one at a time, in few registers)
+          }
+        }
         y = __builtin_bit_cast(words, out);
       }
       T *out;
@@ -343,7 +389,8 @@ __global__ __launch_bounds__(BLOCK, sizeof(T) == 2 ? 8 : 4) void append_whole(Ap
 }
 
 // From here on a wave takes a token by itself: 256 CUs hold as many waves at eight a SIMD.
-// The 70B shape, one wave and four: 4,096 tokens 54 and 41 us, 8,192 tokens 71 and 76.
+// The 70B shape, one wave and four: 2,048 tokens 41 and 27 us, 4,096 54 and 45, 8,192 76 and
+// 85, 16,384 148 and 164.
 constexpr int kManyTokens = 8192;
 
 }  // namespace

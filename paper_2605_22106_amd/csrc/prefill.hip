@@ -566,8 +566,7 @@ struct Cfg {
   static constexpr int KEYS = 16 * SUBS;
   static constexpr int NS = KEYS / 32;                   // 32-key tiles of S
   static constexpr int BUF = KEYS * ROW;                 // K (or V) of a step
-  static constexpr int LPW = SUBS * 2 * 16 * ROW / 1024 / kWaves;   // 1 KB loads of a wave
-  static constexpr int LPS = 16 * ROW / 1024;            // of a sub-page
+  static constexpr int LPS = 16 * ROW / 1024;            // 1 KB loads of a sub-page
   static constexpr int DT = D / 32;
   static constexpr int NQ = ROW / 32;                    // 16-byte operand pieces of a lane
   static constexpr int LDS = 4 * BUF;
