@@ -580,9 +580,9 @@ int arbor_fork(const arbor_geom_t *geom, arbor_tree_t *tree, arbor_pool_t *pool,
  * inv_freq[j], j < rotary_dim / 2, the pair (y_a, y_b) becomes
  *   (y_a cos a_j - y_b sin a_j,  y_b cos a_j + y_a sin a_j),
  * (a, b) = (j, j + rotary_dim / 2), or (2j, 2j + 1) when interleaved = 1; elements
- * from rotary_dim on stay.  Angles are formed in 64 bits, the rest in fp32 (where
- * pairs are neighbours or halves of the whole head, a bf16 result that fp32 does not
- * decide in 64 bits too), and each result is rounded once.  Queries go to q_out [n_tokens][Hq][head_dim]; keys
+ * from rotary_dim on stay.  Angles are formed in 64 bits, the rest in fp32 (a bf16
+ * result that fp32 does not decide in 64 bits too), and each result is rounded once.
+ * Queries go to q_out [n_tokens][Hq][head_dim]; keys
  * and values (values unchanged) to row slots[t] of layer `layer` of the pool, and,
  * where a record is given, to row tokens[t] of it ([N][L][Hkv][head_dim], the
  * token-span record that arbor_rehydrate reads; pinned host or device).  A token

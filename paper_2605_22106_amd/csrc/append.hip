@@ -80,8 +80,21 @@ __device__ __forceinline__ void sin_cos_turns(double x, F *s, F *c) {
 
 // A bf16 result is formed again in 64 bits where its fp32 value lies within so many last
 // places of the middle between two bf16: the roundings of the norm's factor (three), of
-// sine and cosine, and of two products, a sum and the result are less than that together.
+// sine and cosine, and of two products, a sum and the result are less than that together,
+// but for sums that cancel to less than half of their terms.
 constexpr uint32_t kTie = 6;
+
+// how far beyond kTie below a middle, in last places: decided by fp32 above 2 kTie
+__device__ __forceinline__ uint32_t beyond_tie(float f) {
+  return (__builtin_bit_cast(uint32_t, f) - (0x8000 - kTie)) & 0xffff;
+}
+// rounded to fp32 and to T, as fp32 arithmetic without an error would be
+template <class T>
+__device__ __forceinline__ T by_fp32(double v) {
+  float f = (float)v;
+  asm volatile("" : "+v"(f));
+  return (T)f;
+}
 
 // 1 / sqrt(x) by the instruction, good to 2^-23 or so, and two steps of Newton's method
 __device__ __forceinline__ double inverse_root(double x) {
@@ -90,13 +103,14 @@ __device__ __forceinline__ double inverse_root(double x) {
   return r > 0.0 && r < 1.0e300 ? m : r;        // (0 of an infinity, infinity of 0)
 }
 
+// Part of a head rotated by halves; see above.
 template <class T, int D>
 __global__ __launch_bounds__(256) void append_rows(AppendArgs args) {
   constexpr int LPR = D / 8;                    // lanes of a head
   constexpr int RPS = 256 / LPR;                // heads a step
   constexpr int UNROLL = 4;                     // steps whose loads are in flight together
   typedef typename Piece<T>::reg reg;
-  __shared__ float sh_cos[D / 2], sh_sin[D / 2];
+  __shared__ double sh_cos[D / 2], sh_sin[D / 2];
   const arbor_append_t &a = args.a;
   const Pool &pl = args.pl;
   if (status_failed(args.status)) return;
@@ -111,9 +125,8 @@ __global__ __launch_bounds__(256) void append_rows(AppendArgs args) {
   }
   const int tid = threadIdx.x, q8 = tid % LPR;
   const int rd = a.rotary_dim, half = rd / 2;
-  const bool split = !a.interleaved && q8 < rd / 8;    // this lane's pieces lie half apart
-  const int ca = split ? 4 * q8 : 8 * q8, cb = split ? half + 4 * q8 : 8 * q8 + 4;
-  const bool turns = q8 < rd / 8;
+  const bool turns = q8 < rd / 8;               // this lane's pieces lie half apart
+  const int ca = turns ? 4 * q8 : 8 * q8, cb = turns ? half + 4 * q8 : 8 * q8 + 4;
   const int Hq = pl.Hkv * pl.G, heads = Hq + 2 * pl.Hkv;
   auto row_of = [&](int h) -> const T * {
     const T *p = static_cast<const T *>(h < Hq ? a.q : h < Hq + pl.Hkv ? a.k : a.v);
@@ -136,22 +149,17 @@ __global__ __launch_bounds__(256) void append_rows(AppendArgs args) {
   };
   int h0 = tid / LPR;
   load(h0);
-  if (rd > 0) {
-    if (tid < half) {
-      // in turns: x = pos f / (2 pi) in fp64 is off by 2^-53 relative, 1e-10 turns
-      // at position 10^6
-      sin_cos_turns((double)a.positions[t] * (double)a.inv_freq[tid] * 0.15915494309189535,
-                    &sh_sin[tid], &sh_cos[tid]);
-    }
-    __syncthreads();
-  }
-  // elements (a, b) of pair e of this lane: split (xa[e], xb[e]); otherwise
-  // (xa[0], xa[1]), (xa[2], xa[3]), (xb[0], xb[1]), (xb[2], xb[3]): pair 4 q8 + e either way
-  float co[4], si[4];
+  // in turns: x = pos f / (2 pi) in fp64 is off by 2^-53 relative, 1e-10 turns at position
+  // 10^6
+  if (tid < half)
+    sin_cos_turns((double)a.positions[t] * (double)a.inv_freq[tid] * 0.15915494309189535,
+                  &sh_sin[tid], &sh_cos[tid]);
+  __syncthreads();
+  float co[4], si[4];                           // of the pairs (xa[e], xb[e])
 #pragma unroll
   for (int e = 0; e < 4; ++e) {
-    co[e] = turns ? sh_cos[4 * q8 + e] : 1.0f;
-    si[e] = turns ? sh_sin[4 * q8 + e] : 0.0f;
+    co[e] = turns ? (float)sh_cos[4 * q8 + e] : 1.0f;
+    si[e] = turns ? (float)sh_sin[4 * q8 + e] : 0.0f;
   }
   const int64_t page = slot / pl.P, row = slot % pl.P;
   for (; h0 < heads; h0 += UNROLL * RPS) {
@@ -185,25 +193,32 @@ __global__ __launch_bounds__(256) void append_rows(AppendArgs args) {
             vb[e] *= (float)wb[e];
           }
         }
-        if (split) {
+        uint32_t near = ~0u;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const float f = r * (turns ? va[e] * co[e] - vb[e] * si[e] : va[e]);
+          const float g = r * (turns ? vb[e] * co[e] + va[e] * si[e] : vb[e]);
+          ya[e] = (T)f;
+          yb[e] = (T)g;
+          near = min(near, min(beyond_tie(f), beyond_tie(g)));
+        }
+        if (sizeof(T) == 2 && __builtin_expect(ballot(near <= 2 * kTie) != 0, 0)) {
+          double x = 1.0;
+          if (w) {
+            float ss = 0.0f;                         // (of exact squares)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const float p = (float)xa[u][e], q = (float)xb[u][e];
+              ss += p * p + q * q;
+            }
+            x = inverse_root(row_sum<LPR>((double)ss) * (1.0 / D) + a.eps);
+          }
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
-            ya[e] = (T)(r * (va[e] * co[e] - vb[e] * si[e]));
-            yb[e] = (T)(r * (vb[e] * co[e] + va[e] * si[e]));
-          }
-        } else if (turns) {
-#pragma unroll
-          for (int e = 0; e < 2; ++e) {
-            ya[2 * e] = (T)(r * (va[2 * e] * co[e] - va[2 * e + 1] * si[e]));
-            ya[2 * e + 1] = (T)(r * (va[2 * e + 1] * co[e] + va[2 * e] * si[e]));
-            yb[2 * e] = (T)(r * (vb[2 * e] * co[2 + e] - vb[2 * e + 1] * si[2 + e]));
-            yb[2 * e + 1] = (T)(r * (vb[2 * e + 1] * co[2 + e] + vb[2 * e] * si[2 + e]));
-          }
-        } else {
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            ya[e] = (T)(r * va[e]);
-            yb[e] = (T)(r * vb[e]);
+            const double c = turns ? sh_cos[4 * q8 + e] : 1.0, s = sh_sin[turns ? 4 * q8 + e : 0];
+            const double p = va[e], q = vb[e];       // (exact)
+            ya[e] = by_fp32<T>(x * (turns ? fma(-q, s, p * c) : p));
+            yb[e] = by_fp32<T>(x * (turns ? fma(p, s, q * c) : q));
           }
         }
       }
@@ -343,7 +358,7 @@ __global__ __launch_bounds__(BLOCK, BLOCK == 64 && sizeof(T) == 2 ? 8 : 4) void 
           const float s = near_sin[pair(e)];
           const float f = r * (turns ? v[e] * near_cos[pair(e)] + p[e] * (first(e) ? -s : s) : v[e]);
           out.e[e] = (T)f;
-          near = min(near, (__builtin_bit_cast(uint32_t, f) - (0x8000 - kTie)) & 0xffff);
+          near = min(near, beyond_tie(f));
         }
         if (sizeof(T) == 2 && __builtin_expect(ballot(near <= 2 * kTie) != 0, 0)) {
           // (one step of eight; v and p are exact)
@@ -362,9 +377,7 @@ __global__ __launch_bounds__(BLOCK, BLOCK == 64 && sizeof(T) == 2 ? 8 : 4) void 
               const double s = sh_sin[pair(e)];
               y = fma((double)p[e], first(e) ? -s : s, y * sh_cos[pair(e)]);
             }
-            float f = (float)(y * x);
-            asm volatile("" : "+v"(f));
-            out.e[e] = (T)f;
+            out.e[e] = by_fp32<T>(y * x);
             __builtin_amdgcn_sched_barrier(0);       // (one at a time, in few registers)
           }
         }
