@@ -78,15 +78,39 @@ __device__ __forceinline__ void sin_cos_turns(double x, F *s, F *c) {
   *c = (quarter + 1) & 2 ? -v : v;
 }
 
-// A bf16 result is formed again in 64 bits where its fp32 value lies within so many last
-// places of the middle between two bf16: the roundings of the norm's factor (three), of
-// sine and cosine, and of two products, a sum and the result are less than that together,
-// but for sums that cancel to less than half of their terms.
-constexpr uint32_t kTie = 6;
+// A bf16 result is formed again in 64 bits where fp32 does not decide it: where the value
+// and kOff of its terms' magnitudes more, and as much less, round to different bf16.  In
+// units of 2^-24 of r (|y_a cos| + |y_b sin|), r the norm's factor: r is off by at most 6
+// (seven additions of exact squares and one of eps, halved by the root, which adds 2), sine
+// and cosine by 1, one product and the sum by 1 each, the product with r by 1, the two ends
+// by 1; 12 covers their products too.  Where the terms cancel, that is many last places of
+// the result.
+constexpr float kOff = 12.0f * 0x1p-24f;
 
-// how far beyond kTie below a middle, in last places: decided by fp32 above 2 kTie
-__device__ __forceinline__ uint32_t beyond_tie(float f) {
-  return (__builtin_bit_cast(uint32_t, f) - (0x8000 - kTie)) & 0xffff;
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+
+// The values f, which may be off by d, rounded; the bits in which the rounded ends of
+// [f - d, f + d] differ are added to `open`.
+__device__ __forceinline__ bf16x2 rounded(f32x2 f, f32x2 d, uint32_t *open) {
+  const bf16x2 lo = __builtin_convertvector(f - d, bf16x2);
+  const bf16x2 hi = __builtin_convertvector(f + d, bf16x2);
+  *open |= __builtin_bit_cast(uint32_t, lo) ^ __builtin_bit_cast(uint32_t, hi);
+  return lo;
+}
+// Sum of the squares of eight elements, exact for bf16 but for the additions, in pairs.
+__device__ __forceinline__ float squares(const float (&v)[8]) {
+  float s[4];
+#pragma unroll
+  for (int e = 0; e < 4; ++e)
+    s[e] = __builtin_fmaf(v[2 * e], v[2 * e], v[2 * e + 1] * v[2 * e + 1]);
+  return (s[0] + s[1]) + (s[2] + s[3]);
+}
+__device__ __forceinline__ double squares_64(const float (&v)[8]) {
+  double s = 0.0;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) s = fma((double)v[e], (double)v[e], s);
+  return s;
 }
 // rounded to fp32 and to T, as fp32 arithmetic without an error would be
 template <class T>
@@ -94,6 +118,15 @@ __device__ __forceinline__ T by_fp32(double v) {
   float f = (float)v;
   asm volatile("" : "+v"(f));
   return (T)f;
+}
+
+// 1 / sqrt(x), within 2^-23: for bf16 rows by the instruction, which takes an x below the
+// normal range for 0
+template <class T>
+__device__ __forceinline__ float norm_factor(float x) {
+  if constexpr (sizeof(T) == 4) return 1.0f / sqrtf(x);
+  const bool tiny = x < 0x1p-100f;
+  return __builtin_amdgcn_rsqf(tiny ? x * 0x1p100f : x) * (tiny ? 0x1p50f : 1.0f);
 }
 
 // 1 / sqrt(x) by the instruction, good to 2^-23 or so, and two steps of Newton's method
@@ -180,11 +213,8 @@ __global__ __launch_bounds__(256) void append_rows(AppendArgs args) {
         const void *w = is_q ? a.q_norm : a.k_norm;
         float r = 1.0f;
         if (w) {
-          float ss = 0.0f;
-#pragma unroll
-          for (int e = 0; e < 4; ++e) ss += va[e] * va[e] + vb[e] * vb[e];
-          ss = row_sum<LPR>(ss);
-          r = 1.0f / sqrtf(ss * (1.0f / D) + a.eps);
+          const float all[8] = {va[0], va[1], va[2], va[3], vb[0], vb[1], vb[2], vb[3]};
+          r = norm_factor<T>(row_sum<LPR>(squares(all)) * (1.0f / D) + a.eps);
           const reg wa = *reinterpret_cast<const reg *>(static_cast<const T *>(w) + ca);
           const reg wb = *reinterpret_cast<const reg *>(static_cast<const T *>(w) + cb);
 #pragma unroll
@@ -193,25 +223,33 @@ __global__ __launch_bounds__(256) void append_rows(AppendArgs args) {
             vb[e] *= (float)wb[e];
           }
         }
-        uint32_t near = ~0u;
+        uint32_t open = 0;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const float f = r * (turns ? va[e] * co[e] - vb[e] * si[e] : va[e]);
-          const float g = r * (turns ? vb[e] * co[e] + va[e] * si[e] : vb[e]);
-          ya[e] = (T)f;
-          yb[e] = (T)g;
-          near = min(near, min(beyond_tie(f), beyond_tie(g)));
+        for (int e = 0; e < 4; e += 2) {
+          f32x2 f, g, df, dg;
+#pragma unroll
+          for (int i = 0; i < 2; ++i) {
+            const float x = va[e + i], y = vb[e + i], c = co[e + i], s = si[e + i];
+            const float ys = y * s, xs = x * s;
+            f[i] = r * (turns ? __builtin_fmaf(x, c, -ys) : x);
+            g[i] = r * (turns ? __builtin_fmaf(y, c, xs) : y);
+            df[i] = kOff * r * (turns ? __builtin_fmaf(fabsf(x), fabsf(c), fabsf(ys)) : fabsf(x));
+            dg[i] = kOff * r * (turns ? __builtin_fmaf(fabsf(y), fabsf(c), fabsf(xs)) : fabsf(y));
+          }
+          if constexpr (sizeof(T) == 2) {
+            const bf16x2 wa = rounded(f, df, &open), wb = rounded(g, dg, &open);
+            ya[e] = wa[0], ya[e + 1] = wa[1], yb[e] = wb[0], yb[e + 1] = wb[1];
+          } else {
+            ya[e] = f[0], ya[e + 1] = f[1], yb[e] = g[0], yb[e + 1] = g[1];
+          }
         }
-        if (sizeof(T) == 2 && __builtin_expect(ballot(near <= 2 * kTie) != 0, 0)) {
+        if (sizeof(T) == 2 && __builtin_expect(ballot(open != 0) != 0, 0)) {
           double x = 1.0;
           if (w) {
-            float ss = 0.0f;                         // (of exact squares)
+            float all[8];
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              const float p = (float)xa[u][e], q = (float)xb[u][e];
-              ss += p * p + q * q;
-            }
-            x = inverse_root(row_sum<LPR>((double)ss) * (1.0 / D) + a.eps);
+            for (int e = 0; e < 4; ++e) all[e] = (float)xa[u][e], all[4 + e] = (float)xb[u][e];
+            x = inverse_root(row_sum<LPR>(squares_64(all)) * (1.0 / D) + a.eps);
           }
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
@@ -246,14 +284,16 @@ __global__ __launch_bounds__(256) void append_rows(AppendArgs args) {
 // next load as soon as they are read; where a wave takes a token by itself two in flight,
 // with the sines read from LDS, leave eight waves to a SIMD (six: 87 us and more).  Each
 // line is read once and written once, past the caches (7 us more with ordinary stores).
-// 8,192 tokens of 64 + 8 + 8 heads of 128 bf16, 336 MB: 76 us, 4.4 TB/s of the 5.1 of a
+// 8,192 tokens of 64 + 8 + 8 heads of 128 bf16, 336 MB: 79 us, 4.3 TB/s of the 5.1 of a
 // large copy.
 //
 // A bf16 that fp32 rounds to the other side moves its key's logits by up to 2^-8 of a
-// product, so the few results that fp32 does not decide are formed again in 64 bits (2 us
-// of the 76; all of them in 64 bits: 94 us and more).
+// product, so the few pairs of elements that fp32 does not decide are formed again in 64 bits
+// (2 to 5 us of the 79; where one of a lane's eight brought on all of them, 10 to 12; all
+// elements of all rows, 18 and more).
 template <class T, int D, bool HALVES, int BLOCK>
-__global__ __launch_bounds__(BLOCK, BLOCK == 64 && sizeof(T) == 2 ? 8 : 4) void append_whole(AppendArgs args) {
+__global__ __launch_bounds__(BLOCK, BLOCK == 64 && sizeof(T) == 2 ? 8 : 4) void append_whole(
+    AppendArgs args) {
   constexpr int LPR = D / 8;                    // lanes of a head
   constexpr int RPS = BLOCK / LPR;              // heads a step
   constexpr int UNROLL = BLOCK == 64 ? 2 : 4;   // steps whose loads are in flight together
@@ -335,11 +375,7 @@ __global__ __launch_bounds__(BLOCK, BLOCK == 64 && sizeof(T) == 2 ? 8 : 4) void 
         const T *w = static_cast<const T *>(is_q ? a.q_norm : a.k_norm);
         float r = 1.0f;
         if (w) {
-          float ss = 0.0f;
-#pragma unroll
-          for (int e = 0; e < 8; ++e) ss += v[e] * v[e];
-          ss = row_sum<LPR>(ss);
-          r = 1.0f / sqrtf(ss * (1.0f / D) + a.eps);
+          r = norm_factor<T>(row_sum<LPR>(squares(v)) * (1.0f / D) + a.eps);
           const int c = 8 * q8;
           const Eight wo = __builtin_bit_cast(Eight, *reinterpret_cast<const words *>(w + c));
           const Eight wf = __builtin_bit_cast(
@@ -351,33 +387,47 @@ __global__ __launch_bounds__(BLOCK, BLOCK == 64 && sizeof(T) == 2 ? 8 : 4) void 
           }
         }
         Eight out;
-        uint32_t near = ~0u;
+        uint32_t open[4] = {0, 0, 0, 0};
         asm volatile("" ::: "memory");   // (the sines are read here, not kept in registers)
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          const float s = near_sin[pair(e)];
-          const float f = r * (turns ? v[e] * near_cos[pair(e)] + p[e] * (first(e) ? -s : s) : v[e]);
-          out.e[e] = (T)f;
-          near = min(near, beyond_tie(f));
+        for (int e = 0; e < 8; e += 2) {
+          f32x2 f, d;
+#pragma unroll
+          for (int i = 0; i < 2; ++i) {
+            const float c = near_cos[pair(e + i)], s = near_sin[pair(e + i)], y = v[e + i];
+            const float t = p[e + i] * (first(e + i) ? -s : s);
+            f[i] = r * (turns ? __builtin_fmaf(y, c, t) : y);
+            d[i] = kOff * r * (turns ? __builtin_fmaf(fabsf(y), fabsf(c), fabsf(t)) : fabsf(y));
+          }
+          if constexpr (sizeof(T) == 2) {
+            const bf16x2 w2 = rounded(f, d, &open[e / 2]);
+            out.e[e] = w2[0], out.e[e + 1] = w2[1];
+            if (e == 2) __builtin_amdgcn_sched_barrier(0);   // (half the sines at a time)
+          } else {
+            out.e[e] = f[0], out.e[e + 1] = f[1];
+          }
         }
-        if (sizeof(T) == 2 && __builtin_expect(ballot(near <= 2 * kTie) != 0, 0)) {
-          // (one step of eight; v and p are exact)
+        if (sizeof(T) == 2 &&
+            __builtin_expect(ballot((open[0] | open[1] | open[2] | open[3]) != 0) != 0, 0)) {
+          // (v and p are exact)
           asm volatile("" ::: "memory");
           double x = 1.0;
           if (w) {
-            float ss = 0.0f;                         // (of exact squares)
+            float all[8];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) ss += (float)own.e[e] * (float)own.e[e];
-            x = inverse_root(row_sum<LPR>((double)ss) * (1.0 / D) + a.eps);
+            for (int e = 0; e < 8; ++e) all[e] = (float)own.e[e];
+            x = inverse_root(row_sum<LPR>(squares_64(all)) * (1.0 / D) + a.eps);
           }
 #pragma unroll
           for (int e = 0; e < 8; ++e) {
-            double y = v[e];
-            if (turns) {
-              const double s = sh_sin[pair(e)];
-              y = fma((double)p[e], first(e) ? -s : s, y * sh_cos[pair(e)]);
+            if (ballot(open[e / 2] != 0)) {
+              double y = v[e];
+              if (turns) {
+                const double s = sh_sin[pair(e)];
+                y = fma((double)p[e], first(e) ? -s : s, y * sh_cos[pair(e)]);
+              }
+              out.e[e] = by_fp32<T>(y * x);
             }
-            out.e[e] = by_fp32<T>(y * x);
             __builtin_amdgcn_sched_barrier(0);       // (one at a time, in few registers)
           }
         }
