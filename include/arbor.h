@@ -591,8 +591,9 @@ int arbor_fork(const arbor_geom_t *geom, arbor_tree_t *tree, arbor_pool_t *pool,
  * they may be parts of one product's rows); q_out may be q itself where q_stride
  * is Hq * head_dim.  No two tokens may have the same slot.
  * Errors: EINVAL (arguments, a slot outside the pool or, with a record, a token
- * outside [0, N): that token is left out), EUNSUPPORTED (rotary_dim not a multiple
- * of 8 or above head_dim; a pointer or stride that is not a multiple of 16 bytes).
+ * outside [0, N): that token is left out, and any other may be: each is written
+ * whole or not at all), EUNSUPPORTED (rotary_dim not a multiple of 8 or above
+ * head_dim; a pointer or stride that is not a multiple of 16 bytes).
  */
 typedef struct {
   const void *q, *k, *v;            /* device, dtype                                  */

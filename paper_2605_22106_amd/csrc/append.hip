@@ -136,6 +136,62 @@ __device__ __forceinline__ double inverse_root(double x) {
   return r > 0.0 && r < 1.0e300 ? m : r;        // (0 of an infinity, infinity of 0)
 }
 
+// What a token has, loaded in one round trip beside its first rows.
+struct Token {
+  int64_t slot, rec;
+  int32_t pos;
+  float freq;                                   // of pair tid
+  int32_t status;
+};
+__device__ __forceinline__ Token load_token(const AppendArgs &args, int64_t t, int tid) {
+  const arbor_append_t &a = args.a;
+  const int half = a.rotary_dim / 2;
+  // (no branches: what is not needed is read from where something else lies)
+  const float *freq = half > 0 ? a.inv_freq + min(tid, half - 1)
+                               : reinterpret_cast<const float *>(a.positions);
+  Token k;
+  k.status = status_word(args.status);
+  k.freq = *freq;
+  k.slot = a.slots[t];
+  k.rec = (a.record_k ? a.tokens : a.slots)[t];
+  k.pos = a.positions[t];
+  return k;
+}
+// Whether the token has a place; it is left out if not, and refused unless it is padding.
+__device__ __forceinline__ bool has_place(const AppendArgs &args, Token &k, int tid) {
+  const bool record = args.a.record_k != nullptr;
+  asm volatile("" : "+s"(k.slot), "+s"(k.rec), "+s"(k.pos));   // (no load moves below)
+  if (k.slot == -1) return false;
+  if (k.slot < 0 || k.slot >= args.pl.num_pages * args.pl.P ||
+      (record && (k.rec < 0 || k.rec >= args.num_tokens))) {
+    if (tid == 0) status_error(args.status, ARBOR_EINVAL);
+    return false;
+  }
+  return true;
+}
+
+// Token t's rows of q, k and v as heads 0, 1, .. of one row: where the next tensor begins,
+// its distance is added.  (Of a choice between the arguments the compiler makes loads of
+// what each lane needs from the arguments in memory.)
+template <class T, int D>
+struct Heads {
+  const char *q;
+  int64_t to_k, to_v;
+  int hq, hkv;
+  __device__ __forceinline__ Heads(const arbor_append_t &a, const Pool &pl, int64_t t)
+      : hq(pl.Hkv * pl.G), hkv(pl.Hkv) {
+    q = reinterpret_cast<const char *>(static_cast<const T *>(a.q) + t * a.q_stride);
+    const char *k = reinterpret_cast<const char *>(static_cast<const T *>(a.k) + t * a.k_stride);
+    const char *v = reinterpret_cast<const char *>(static_cast<const T *>(a.v) + t * a.v_stride);
+    to_k = (k - q) - (int64_t)hq * (D * sizeof(T));
+    to_v = (v - k) - (int64_t)hkv * (D * sizeof(T));
+  }
+  __device__ __forceinline__ const T *operator[](int h) const {
+    return reinterpret_cast<const T *>(q + (int64_t)h * (D * sizeof(T)) + (h >= hq ? to_k : 0) +
+                                       (h >= hq + hkv ? to_v : 0));
+  }
+};
+
 // Part of a head rotated by halves; see above.
 template <class T, int D>
 __global__ __launch_bounds__(256) void append_rows(AppendArgs args) {
@@ -144,59 +200,51 @@ __global__ __launch_bounds__(256) void append_rows(AppendArgs args) {
   constexpr int UNROLL = 4;                     // steps whose loads are in flight together
   typedef typename Piece<T>::reg reg;
   __shared__ double sh_cos[D / 2], sh_sin[D / 2];
+  __shared__ int32_t sh_status;
   const arbor_append_t &a = args.a;
   const Pool &pl = args.pl;
-  if (status_failed(args.status)) return;
   const int64_t t = blockIdx.x;
-  const int64_t slot = a.slots[t];
-  if (slot == -1) return;
-  const int64_t rec = a.record_k ? a.tokens[t] : 0;
-  if (slot < 0 || slot >= pl.num_pages * pl.P || rec < 0 ||
-      (a.record_k && rec >= args.num_tokens)) {
-    if (threadIdx.x == 0) status_error(args.status, ARBOR_EINVAL);
-    return;
-  }
   const int tid = threadIdx.x, q8 = tid % LPR;
   const int rd = a.rotary_dim, half = rd / 2;
   const bool turns = q8 < rd / 8;               // this lane's pieces lie half apart
   const int ca = turns ? 4 * q8 : 8 * q8, cb = turns ? half + 4 * q8 : 8 * q8 + 4;
   const int Hq = pl.Hkv * pl.G, heads = Hq + 2 * pl.Hkv;
-  auto row_of = [&](int h) -> const T * {
-    const T *p = static_cast<const T *>(h < Hq ? a.q : h < Hq + pl.Hkv ? a.k : a.v);
-    const int64_t stride = h < Hq ? a.q_stride : h < Hq + pl.Hkv ? a.k_stride : a.v_stride;
-    const int hh = h < Hq ? h : h < Hq + pl.Hkv ? h - Hq : h - Hq - pl.Hkv;
-    return p + t * stride + (int64_t)hh * D;
-  };
-  // the first heads' loads are on their way while the angles are formed
+  const Heads<T, D> rows(a, pl, t);
+  // the first heads' loads are on their way while the angles are formed (without a branch,
+  // behind which the compiler would wait for all of them)
   reg xa[UNROLL], xb[UNROLL];
-  auto load = [&](int h0) {
+  auto load = [&](int h0, int last) {
 #pragma unroll
     for (int u = 0; u < UNROLL; ++u) {
-      const int h = h0 + u * RPS;
+      const int h = min(h0 + u * RPS, last);
       if (h < heads) {
-        const T *p = row_of(h);
+        const T *p = rows[h];
         xa[u] = *reinterpret_cast<const reg *>(p + ca);
         xb[u] = *reinterpret_cast<const reg *>(p + cb);
       }
     }
   };
   int h0 = tid / LPR;
-  load(h0);
+  Token k = load_token(args, t, tid);
+  load(h0, heads - 1);
+  if (!has_place(args, k, tid)) return;
   // in turns: x = pos f / (2 pi) in fp64 is off by 2^-53 relative, 1e-10 turns at position
   // 10^6
   if (tid < half)
-    sin_cos_turns((double)a.positions[t] * (double)a.inv_freq[tid] * 0.15915494309189535,
-                  &sh_sin[tid], &sh_cos[tid]);
+    sin_cos_turns((double)k.pos * (double)k.freq * 0.15915494309189535, &sh_sin[tid],
+                  &sh_cos[tid]);
+  if (tid == 0) sh_status = k.status;
   __syncthreads();
+  if (sh_status < 0) return;
   float co[4], si[4];                           // of the pairs (xa[e], xb[e])
 #pragma unroll
   for (int e = 0; e < 4; ++e) {
     co[e] = turns ? (float)sh_cos[4 * q8 + e] : 1.0f;
     si[e] = turns ? (float)sh_sin[4 * q8 + e] : 0.0f;
   }
-  const int64_t page = slot / pl.P, row = slot % pl.P;
+  const int64_t page = k.slot / pl.P, row = k.slot % pl.P;
   for (; h0 < heads; h0 += UNROLL * RPS) {
-    if (h0 >= UNROLL * RPS) load(h0);
+    if (h0 >= UNROLL * RPS) load(h0, INT32_MAX);
 #pragma unroll
     for (int u = 0; u < UNROLL; ++u) {
       const int h = h0 + u * RPS;
@@ -269,7 +317,7 @@ __global__ __launch_bounds__(256) void append_rows(AppendArgs args) {
                                     row_byte_offset(pl, args.layer, page, g, (int)row));
         if (a.record_k) {
           T *r = static_cast<T *>(is_v ? a.record_v : a.record_k) +
-                 ((rec * pl.L + args.layer) * pl.Hkv + g) * D;
+                 ((k.rec * pl.L + args.layer) * pl.Hkv + g) * D;
           *reinterpret_cast<reg *>(r + ca) = ya;
           *reinterpret_cast<reg *>(r + cb) = yb;
         }
@@ -284,12 +332,12 @@ __global__ __launch_bounds__(256) void append_rows(AppendArgs args) {
 // next load as soon as they are read; where a wave takes a token by itself two in flight,
 // with the sines read from LDS, leave eight waves to a SIMD (six: 87 us and more).  Each
 // line is read once and written once, past the caches (7 us more with ordinary stores).
-// 8,192 tokens of 64 + 8 + 8 heads of 128 bf16, 336 MB: 79 us, 4.3 TB/s of the 5.1 of a
+// 8,192 tokens of 64 + 8 + 8 heads of 128 bf16, 336 MB: 70 us, 4.8 TB/s of the 5.1 of a
 // large copy.
 //
 // A bf16 that fp32 rounds to the other side moves its key's logits by up to 2^-8 of a
 // product, so the few pairs of elements that fp32 does not decide are formed again in 64 bits
-// (2 to 5 us of the 79; where one of a lane's eight brought on all of them, 10 to 12; all
+// (2 to 5 us; where one of a lane's eight brought on all of them, 10 to 12; all
 // elements of all rows, 18 and more).
 template <class T, int D, bool HALVES, int BLOCK>
 __global__ __launch_bounds__(BLOCK, BLOCK == 64 && sizeof(T) == 2 ? 8 : 4) void append_whole(
@@ -304,54 +352,42 @@ __global__ __launch_bounds__(BLOCK, BLOCK == 64 && sizeof(T) == 2 ? 8 : 4) void 
   typedef uint32_t words __attribute__((ext_vector_type(W), aligned(16)));
   __shared__ __attribute__((aligned(16))) double sh_cos[D / 2], sh_sin[D / 2];
   __shared__ __attribute__((aligned(16))) float near_cos[D / 2], near_sin[D / 2];
+  __shared__ int32_t sh_status;
   const arbor_append_t &a = args.a;
   const Pool &pl = args.pl;
   const int64_t t = blockIdx.x;
   const int tid = threadIdx.x, q8 = tid % LPR;
   const int rd = a.rotary_dim, half = rd / 2;
-  // (in one round trip: all that the token has)
-  const bool failed = status_failed(args.status);
-  const int64_t slot = a.slots[t];
-  const int64_t rec = a.record_k ? a.tokens[t] : 0;
-  const int64_t pos = rd > 0 ? a.positions[t] : 0;
-  const double freq = tid < half ? (double)a.inv_freq[tid] : 0.0;
   const int Hq = pl.Hkv * pl.G, heads = Hq + 2 * pl.Hkv;
-  // the first heads' loads are on their way while the angles are formed
+  const Heads<T, D> rows(a, pl, t);
+  // the first heads' loads are on their way while the angles are formed (without a branch,
+  // behind which the compiler would wait for all of them)
   words x[UNROLL];
   auto fetch = [&](int u, int h) {
-    if (h < heads) {
-      const T *p = static_cast<const T *>(h < Hq ? a.q : h < Hq + pl.Hkv ? a.k : a.v);
-      const int64_t stride = h < Hq ? a.q_stride : h < Hq + pl.Hkv ? a.k_stride : a.v_stride;
-      const int hh = h < Hq ? h : h < Hq + pl.Hkv ? h - Hq : h - Hq - pl.Hkv;
-      x[u] = __builtin_nontemporal_load(
-          reinterpret_cast<const words *>(p + t * stride + (int64_t)hh * D + 8 * q8));
-    }
+    if (h < heads)
+      x[u] = __builtin_nontemporal_load(reinterpret_cast<const words *>(rows[h] + 8 * q8));
   };
   int h0 = tid / LPR;
+  Token k = load_token(args, t, tid);
 #pragma unroll
-  for (int u = 0; u < UNROLL; ++u) fetch(u, h0 + u * RPS);
-  if (failed || slot == -1) return;
-  if (slot < 0 || slot >= pl.num_pages * pl.P || rec < 0 ||
-      (a.record_k && rec >= args.num_tokens)) {
-    if (tid == 0) status_error(args.status, ARBOR_EINVAL);
-    return;
+  for (int u = 0; u < UNROLL; ++u) fetch(u, min(h0 + u * RPS, heads - 1));
+  if (!has_place(args, k, tid)) return;
+  // in turns: pos f / (2 pi) in fp64 is off by 2^-53 relative, 1e-10 turns at position
+  // 10^6
+  if (tid < half) {
+    double s, c;
+    sin_cos_turns((double)k.pos * (double)k.freq * 0.15915494309189535, &s, &c);
+    sh_sin[tid] = s, sh_cos[tid] = c;
+    near_sin[tid] = (float)s, near_cos[tid] = (float)c;
   }
-  if (rd > 0) {
-    // in turns: pos f / (2 pi) in fp64 is off by 2^-53 relative, 1e-10 turns at position
-    // 10^6
-    if (tid < half) {
-      double s, c;
-      sin_cos_turns((double)pos * freq * 0.15915494309189535, &s, &c);
-      sh_sin[tid] = s, sh_cos[tid] = c;
-      near_sin[tid] = (float)s, near_cos[tid] = (float)c;
-    }
-    __syncthreads();
-  }
+  if (tid == 0) sh_status = k.status;
+  __syncthreads();
+  if (sh_status < 0) return;
   // element e becomes own co + partner si
   const bool turns = 8 * q8 < rd;
   auto pair = [&](int e) { return HALVES ? (8 * q8 + e) & (D / 2 - 1) : 4 * q8 + e / 2; };
   auto first = [&](int e) { return HALVES ? 8 * q8 < half : e % 2 == 0; };
-  const int64_t page = slot / pl.P, row = slot % pl.P;
+  const int64_t page = k.slot / pl.P, row = k.slot % pl.P;
   for (; h0 < heads; h0 += UNROLL * RPS) {
 #pragma unroll
     for (int u = 0; u < UNROLL; ++u) {
@@ -442,7 +478,7 @@ __global__ __launch_bounds__(BLOCK, BLOCK == 64 && sizeof(T) == 2 ? 8 : 4) void 
                                     row_byte_offset(pl, args.layer, page, g, (int)row));
         if (a.record_k) {
           T *r = static_cast<T *>(is_v ? a.record_v : a.record_k) +
-                 ((rec * pl.L + args.layer) * pl.Hkv + g) * D;
+                 ((k.rec * pl.L + args.layer) * pl.Hkv + g) * D;
           *reinterpret_cast<words *>(r + 8 * q8) = y;
         }
       }

@@ -68,6 +68,12 @@ __device__ __forceinline__ bool status_failed(const int32_t *st) {
   // a flat one)
   return *(const __attribute__((address_space(1))) volatile int32_t *)st < 0;
 }
+// The status word without a wait for it, where other loads are on their way too.  A launch
+// whose other workgroups may raise an error acts on one read of it for the workgroup.
+__device__ __forceinline__ int32_t status_word(const int32_t *st) {
+  return __hip_atomic_load((const __attribute__((address_space(1))) int32_t *)st, __ATOMIC_RELAXED,
+                           __HIP_MEMORY_SCOPE_AGENT);
+}
 __device__ __forceinline__ void status_error(int32_t *st, int32_t code) { atomicMin(st, code); }
 __device__ __forceinline__ void status_warn(int32_t *st, int32_t code) { atomicCAS(st, 0, code); }
 
