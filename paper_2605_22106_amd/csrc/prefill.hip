@@ -253,8 +253,10 @@ __device__ int walk_chain(const int32_t *parent, int x, C *chain, int col) {
 // Tile k's chain blocks, and its tokens' own slots; one wave.  Lane j's sequence has its
 // chain, `depth` blocks, in column col.  Blocks come in ascending order of ids, so the next
 // one is the smallest id that any lane has next; 64 of them wait in the lanes.
+// False if a block has more slots to see than pages: so every entry's slots lie within the
+// page table.
 template <class C, class O>
-__device__ void merge_chains(const int32_t *n_kept, const O *page_off, const int32_t *cu,
+__device__ bool merge_chains(const int32_t *n_kept, const O *page_off, int P, const int32_t *cu,
                              const PlanPtrs &p, int k, Tile *tile, const C *chain, int col,
                              int depth) {
   const int lane = lane_id();
@@ -272,11 +274,14 @@ __device__ void merge_chains(const int32_t *n_kept, const O *page_off, const int
   }
   int subs = 0, n = 0;
   Entry mine{};
+  bool bad = false;
   auto flush = [&](int cnt) {
     int need = 0;
     if (lane < cnt) {
       if (mine.below != mine.own) mine.limit = n_kept[mine.node];
-      mine.po = (int32_t)page_off[mine.node];
+      const int64_t po = page_off[mine.node], end = page_off[mine.node + 1];
+      mine.po = (int32_t)po;
+      bad = bad || mine.limit < 0 || po < 0 || (end - po) * P < mine.limit;
       need = (mine.limit + 15) / 16;
     }
     const int inc = wave_inclusive_scan(need);
@@ -322,6 +327,7 @@ __device__ void merge_chains(const int32_t *n_kept, const O *page_off, const int
     const int l = lane_value(lo, j), h = lane_value(hi, j), last = lane_value(newest, j);
     for (int y = l + lane; y < h; y += kWave) p.tok[y] = int2{last - (h - 1 - y), j};
   }
+  return !ballot(bad);
 }
 
 // Long tiles are cut into parts, and all parts listed, longest first.  Parts are in
@@ -473,7 +479,7 @@ __global__ __launch_bounds__(1024) void plan_small(Tree t, int G, int Hkv, int P
                                                    PlanPtrs p, int target, int min_part,
                                                    int32_t *status) {
   __shared__ int32_t depth[kWave], sh_cu[kWave + 1];
-  __shared__ int32_t sh_parent[kSmallV], sh_kept[kSmallV], sh_page_off[kSmallV];
+  __shared__ int32_t sh_parent[kSmallV], sh_kept[kSmallV], sh_page_off[kSmallV + 1];
   __shared__ uint16_t chain[MAXD * kCol];
   __shared__ Tile tiles[kSmallTiles];
   __shared__ int n_tiles;
@@ -484,6 +490,7 @@ __global__ __launch_bounds__(1024) void plan_small(Tree t, int G, int Hkv, int P
     sh_kept[i] = t.n_kept[i];
     sh_page_off[i] = (int32_t)t.page_off[i];
   }
+  if (threadIdx.x == 0) sh_page_off[t.V] = (int32_t)t.page_off[t.V];
   if (threadIdx.x == 0) p.head->magic = 0;
   if (status_failed(status)) return;
   if (!request_ok(t, nodes, n_seq, cu, n_tokens, sh_cu)) {
@@ -505,10 +512,14 @@ __global__ __launch_bounds__(1024) void plan_small(Tree t, int G, int Hkv, int P
   }
   for (int k = wave; k < n_tiles; k += 16) {
     const int col = min(tiles[k].e0 + lane, kWave - 1);
-    merge_chains(sh_kept, sh_page_off, sh_cu, p, k, &tiles[k], chain, col, depth[col]);
+    if (!merge_chains(sh_kept, sh_page_off, P, sh_cu, p, k, &tiles[k], chain, col, depth[col]))
+      err = ARBOR_EINVAL;
   }
   if (threadIdx.x == 0) write_header(p, t, G, Hkv, P, n_seq, n_tokens, n_tiles);
-  __syncthreads();
+  if (__syncthreads_or(err)) {
+    if (err) status_error(status, err);
+    return;
+  }
   if (n_tiles <= kWave) list_few(p, tiles, n_tiles, target, min_part, status);
   else list_units(p, tiles, n_tiles, target, min_part, status);
 }
@@ -532,16 +543,22 @@ __global__ __launch_bounds__(1024) void plan_tiles(Tree t, int G, int Hkv, int P
                        : cut_tiles(G, n_seq, cu, p.tiles, (int)p.tiles_cap, status);
   if (threadIdx.x == 0) write_header(p, t, G, Hkv, P, n_seq, n_tokens, n);
 }
-__global__ __launch_bounds__(64) void plan_chains(Tree t, const int32_t *__restrict__ nodes,
+__global__ __launch_bounds__(64) void plan_chains(Tree t, int P,
+                                                  const int32_t *__restrict__ nodes,
                                                   const int32_t *__restrict__ cu, PlanPtrs p,
                                                   int32_t *status) {
   __shared__ int32_t chain[MAXD * kCol];
-  if (status_failed(status) || (int)blockIdx.x >= p.head->n_tiles) return;
+  // (one read for the wave: other tiles may raise an error meanwhile)
+  if (__builtin_amdgcn_readfirstlane(status_word(status)) < 0 ||
+      (int)blockIdx.x >= p.head->n_tiles)
+    return;
   const int lane = lane_id(), e0 = p.tiles[blockIdx.x].e0, ne = p.tiles[blockIdx.x].ne;
   const int d = walk_chain(t.parent, lane < ne ? nodes[e0 + lane] : -1, chain, lane);
   if (d < 0) status_error(status, d);
   if (ballot(d < 0)) return;
-  merge_chains(t.n_kept, t.page_off, cu, p, blockIdx.x, &p.tiles[blockIdx.x], chain, lane, d);
+  if (!merge_chains(t.n_kept, t.page_off, P, cu, p, blockIdx.x, &p.tiles[blockIdx.x], chain, lane,
+                    d) && lane == 0)
+    status_error(status, ARBOR_EINVAL);
 }
 __global__ __launch_bounds__(1024) void plan_units(PlanPtrs p, int target, int min_part,
                                                    int32_t *status) {
@@ -711,10 +728,8 @@ constexpr int kMask = 1 << 16;   // some row of this wave must not see some key 
 constexpr int kNone = 1 << 17;   // no row of this wave sees any
 static_assert(kMaxSeq * MAXD <= 4096, "chain blocks of a tile fit 12 bits");
 
-// (all in one round trip)
-__device__ __forceinline__ bool header_ok(const AttnArgs &a) {
-  const Header h = *a.p.head;
-  const int64_t table = a.t.page_off[a.t.V];
+// Whether the plan, whose header is h, is of this call and tree.
+__device__ __forceinline__ bool header_ok(const AttnArgs &a, const Header &h, int64_t table) {
   return (h.magic == kMagic) & (h.n_seq == a.n_seq) & (h.n_tokens == a.n_tokens) &
          (h.V == a.t.V) & (h.table == table) & (h.G == a.pl.G) & (h.Hkv == a.pl.Hkv) &
          (h.page_size == a.pl.P);
@@ -725,18 +740,22 @@ __global__ __launch_bounds__(kRows * 2, 2) void prefill_attn(AttnArgs a) {
   typedef Cfg<T, D> C;
   extern __shared__ __attribute__((aligned(16))) char lds[];
   __shared__ Entry sh_ent[kEntLds];
+  __shared__ int32_t sh_status;
   const Pool &pl = a.pl;
   const int g = blockIdx.x % pl.Hkv, u = blockIdx.x / pl.Hkv;
   // (in one round trip: the status, the header, and the unit whether there is one or not)
-  const bool failed = status_failed(a.status), ok = header_ok(a);
-  const int n_units = a.p.head->n_units;
-  const Unit un = a.p.units[u];
-  if (failed) return;
-  if (!ok) {
+  const int32_t status = status_word(a.status);
+  Header head_of = *a.p.head;
+  const int64_t table = a.t.page_off[a.t.V];
+  Unit un = a.p.units[u];
+  // (no load moves below the branches)
+  asm volatile("" : "+s"(head_of.n_units), "+s"(un.t0), "+s"(un.nt), "+s"(un.n_ent), "+s"(un.part),
+               "+s"(un.s0), "+s"(un.s1), "+s"(un.ent));
+  if (!header_ok(a, head_of, table)) {
     if (blockIdx.x == 0 && threadIdx.x == 0) status_error(a.status, ARBOR_EINVAL);
     return;
   }
-  if (u >= n_units) return;
+  if (u >= head_of.n_units) return;
   // (global and LDS reads of a block stay apart: a pointer that may be either makes flat
   // loads, which wait for both kinds)
   typedef const __attribute__((address_space(1))) Entry *GlobalEnt;
@@ -779,7 +798,11 @@ __global__ __launch_bounds__(kRows * 2, 2) void prefill_attn(AttnArgs a) {
   const uint64_t seq_bit = live ? 1ull << (info.y & 63) : 0;
   const bool any_live = wave * 32 / G < un.nt;
   if (tid < kEntLds) sh_ent[tid] = staged;
+  // one read of the status decides for the workgroup: others of this launch may find the
+  // plan stale meanwhile
+  if (tid == 0) sh_status = status;
   __syncthreads();
+  if (sh_status < 0) return;
   // sequences and own slots of the wave's rows
   uint64_t seqs = wave_allreduce(seq_bit, [](uint64_t x, uint64_t y) { return x | y; });
   const int qmin = wave_allreduce(live ? qslot : INT32_MAX,
@@ -810,7 +833,7 @@ __global__ __launch_bounds__(kRows * 2, 2) void prefill_attn(AttnArgs a) {
     const int page = a.t.page_table[(int64_t)en.po + slot / pl.P];
     const bool there = page >= 0 && page < pl.num_pages;
     stale = stale || (in && !there);             // the tree has changed since the plan
-    const int valid = in ? min(16, en.limit - slot) : 0;
+    const int valid = in && there ? min(16, en.limit - slot) : 0;
     const uint64_t mine = en.below & seqs, mown = en.own & seqs;
     const bool none = !in || mine == 0 || (mine == mown && slot > qmax);
     const bool mask = mine != seqs || valid < 16 || (mown && slot + 15 > qmin);
@@ -1196,9 +1219,13 @@ __global__ __launch_bounds__(256) void prefill_join(AttnArgs a) {
   const int rows = x % kWaves;                  // 32 rows: the wave that had them
   x /= kWaves;
   const int g = x % pl.Hkv, k = x / pl.Hkv;
-  const int4 tl = a.p.split[min(k, target_parts(pl.Hkv) - 1)];
-  const bool failed = status_failed(a.status), ok = header_ok(a);
-  if (failed || !ok || k >= a.p.head->n_split) return;
+  const int32_t status = status_word(a.status);
+  Header head_of = *a.p.head;
+  const int64_t table = a.t.page_off[a.t.V];
+  int4 tl = a.p.split[min(k, target_parts(pl.Hkv) - 1)];
+  asm volatile("" : "+s"(head_of.n_split), "+s"(tl.x), "+s"(tl.y), "+s"(tl.z), "+s"(tl.w));
+  if (!header_ok(a, head_of, table) | (k >= head_of.n_split)) return;
+  if (status < 0) return;
   const int t0 = tl.x, nt = tl.y, part0 = tl.z, parts = tl.w;
   if (rows * 32 / pl.G >= nt || part0 + parts > a.part_cap) return;
   const int lane = lane_id(), wave = threadIdx.x / kWave, lr = lane & 31, h = lane >> 5;
@@ -1296,8 +1323,8 @@ int launch_prefill_plan(const arbor_geom_t *geom, const arbor_tree_t *tree, cons
   } else {
     hipLaunchKernelGGL(plan_tiles, dim3(1), dim3(1024), 0, stream, t, G, Hkv, P, nodes, n_seq, cu,
                        n_tokens, p, status);
-    hipLaunchKernelGGL(plan_chains, dim3((unsigned)p.tiles_cap), dim3(64), 0, stream, t, nodes, cu,
-                       p, status);
+    hipLaunchKernelGGL(plan_chains, dim3((unsigned)p.tiles_cap), dim3(64), 0, stream, t, P, nodes,
+                       cu, p, status);
     hipLaunchKernelGGL(plan_units, dim3(1), dim3(1024), 0, stream, p, target, min_part,
                        status);
   }

@@ -4,8 +4,10 @@ import pytest
 import torch
 
 from paper_2605_22106_amd import _lib as L
-from tests.gpu_helpers import check_rc, status
+from tests.gpu_helpers import check_rc, status, to_gpu
+from tests.grow_helpers import grow_state, ragged
 from tests.test_gpu_grow import append_case, split
+from tests.test_gpu_prefill import Prefill, queries
 
 pytestmark = pytest.mark.gpu
 
@@ -41,3 +43,43 @@ def test_a_bad_slot_leaves_other_tokens_whole(tokens, rotary, record):
     written = (hit == clean).all(1)
     untouched = (hit == 7.0).all(1)
     assert bool(untouched[bad].all()) and bool((written | untouched).all())
+
+
+@pytest.mark.parametrize("lost", [1.0, 0.02])
+@pytest.mark.parametrize("dtype,head_dim", [("bf16", 128), ("f32", 64)])
+def test_a_stale_plan_of_many_tiles_is_refused(dtype, head_dim, lost):
+    """Some or all pages of the tree have gone since the plan was made: hundreds of workgroups
+    find so, thousands start meanwhile.  The error is raised and the pool stays as it was."""
+    parent = [-1] + [0] * 60
+    n = [4000] + ragged(3, 60, 200, 900)
+    st = grow_state(parent, n, kv_heads=4, q_per_kv=8, head_dim=head_dim, dtype=dtype, layers=1)
+    kv = to_gpu(st)
+    m = [x - 3 for x in n[1:]]
+    pf = Prefill(kv, list(range(1, 61)), m)
+    q = queries(kv, sum(m))
+    gone = torch.rand(kv.page_table.numel(), generator=torch.Generator().manual_seed(1)) < lost
+    kv.page_table[gone.cuda()] = -1
+    before = [x.clone() for x in (kv.k, kv.v, kv.slot_pos)]
+    for _ in range(3):
+        pf.status.zero_()
+        pf(q)
+        assert int(pf.status) == L.EINVAL
+    for x, y in zip((kv.k, kv.v, kv.slot_pos), before):
+        assert torch.equal(x.view(torch.uint8), y.view(torch.uint8))
+
+
+@pytest.mark.parametrize("blocks", [5, 5000])
+def test_a_block_with_more_tokens_than_pages(blocks):
+    """A malformed tree: the plan refuses it, so no entry of the page table beyond the block's
+    is read.  As an ancestor, as the block itself, as the last block."""
+    parent = [-1] + [0] * (blocks - 1)
+    for node, bad, count in ((1, 0, 20 + 40 + 16), (2, 2, 80), (blocks - 1, blocks - 1, 1 << 30),
+                             (1, 0, -1)):
+        st = grow_state(parent, [20] * blocks, kv_heads=1, layers=1)
+        kv = to_gpu(st)
+        kv.n_kept[bad] = count
+        pf = Prefill(kv, [node], [4])
+        assert int(pf.status) == L.EINVAL, (node, bad)
+        pf.status.zero_()
+        pf(queries(kv, 4))                       # a plan that was refused is none
+        assert int(pf.status) == L.EINVAL
