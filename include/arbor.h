@@ -528,7 +528,9 @@ size_t arbor_uncertainty_workspace_size(int32_t n_rows, int64_t vocab, int32_t d
  *                 and its position in its block;
  *   tokens[t]     tok_off[i] + its position in its block, the index of per-token
  *                 arrays (nullable).
- * The rows of the new slots hold nothing yet: arbor_append writes them.
+ * The rows of the new slots hold nothing yet: arbor_append writes them.  Neither
+ * does A, where it is kept: it is 0 at positions that no token has had, or that
+ * arbor_truncate_scored has cleared.
  * Errors: EINVAL (ids, cu, a malformed tree, a block beyond its capacity, n_full
  * not tree->n_full), ENOPAGES, EUNSUPPORTED (a block deeper than
  * ARBOR_MAX_DEPTH), EWORKSPACE.
@@ -546,13 +548,30 @@ int arbor_extend(const arbor_geom_t *geom, arbor_tree_t *tree, arbor_pool_t *poo
  * page-table entries -1, and the freed pages go back on the free stack so that
  * popping them in (node, page) order gives each block its own pages again: an
  * arbor_extend followed by the arbor_truncate that takes its tokens back leaves
- * the free stack as it was.
+ * the free stack as it was.  Accumulated attention is not touched: what A holds at
+ * the positions taken back would be credited to the tokens that get them next.
+ * Where A is kept, arbor_truncate_scored is the call.
  * Errors: EINVAL (ids, a negative keep, n_full not tree->n_full), ECORRUPT (free
  * stack would overflow), EWORKSPACE.
  */
 int arbor_truncate(const arbor_geom_t *geom, arbor_tree_t *tree, arbor_pool_t *pool,
                    int32_t *n_full, const int32_t *nodes, const int32_t *keep, int32_t n_nodes,
                    int32_t *status, void *workspace, size_t workspace_bytes, hipStream_t stream);
+
+/*
+ * arbor_truncate_scored -- arbor_truncate that also clears the accumulated
+ * attention of the tokens taken back: A[tok_off[i] + p] = 0 for min(n_i, keep[e])
+ * <= p < n_i, and rows_seen[i] = 0 for a block that is left empty (a block that
+ * keeps tokens keeps its rows_seen, by which their A is normalised).  Tokens that
+ * arbor_extend then reserves at these positions start from 0.  What the tokens
+ * taken back have credited to others stays.  A is fp32 [N], rows_seen int64 [V].
+ * Errors: those of arbor_truncate; EINVAL for A or rows_seen NULL with n_nodes > 0,
+ * or a block with more tokens than its capacity.
+ */
+int arbor_truncate_scored(const arbor_geom_t *geom, arbor_tree_t *tree, arbor_pool_t *pool,
+                          int32_t *n_full, const int32_t *nodes, const int32_t *keep,
+                          int32_t n_nodes, float *A, int64_t *rows_seen, int32_t *status,
+                          void *workspace, size_t workspace_bytes, hipStream_t stream);
 
 /*
  * arbor_fork -- block dst[e] becomes a copy of block src[e] (a thought that is

@@ -32,7 +32,7 @@ of the paper it follows:
   walk              Alg. 2 (event-driven controller): Transition events to a
                     sequence of active leaves with lazy rehydration, and the
                     Pressure event raised at B - delta
-  extend, truncate, fork, append, prefill_attn
+  extend, truncate, truncate_scored, fork, append, prefill_attn
                     Sec. 3 (blocks are token spans that the search writes,
                     drops and continues in several ways; a token depends on
                     its ancestor chain alone): growing the same paged pool
@@ -784,6 +784,20 @@ def truncate(st, nodes, keep):
         st["free_stack"][int(st["free_top"])] = page
         st["free_top"] = st["free_top"] + 1
     return st, OK
+
+
+def truncate_scored(st, nodes, keep, A, rows_seen):
+    """truncate, with no attention left of the tokens taken back, and no rows seen by a block
+    left empty: (new state, A, rows_seen, status)."""
+    new, status = truncate(st, nodes, keep)
+    A, rows_seen = A.copy(), rows_seen.copy()
+    if status == OK:
+        for i in nodes:
+            n0, n1, at = int(st["n_full"][i]), int(new["n_full"][i]), int(st["tok_off"][i])
+            A[at + n1:at + n0] = 0
+            if n1 == 0:
+                rows_seen[i] = 0
+    return new, A, rows_seen, status
 
 
 def fork(st, src, dst, A=None, rows_seen=None):

@@ -138,6 +138,8 @@ def load() -> ctypes.CDLL:
             "arbor_extend": (ctypes.c_int, [G, T, Pl, vp, vp, i32, vp, i32, vp, vp, vp, vp, vp, sz,
                                             vp]),
             "arbor_truncate": (ctypes.c_int, [G, T, Pl, vp, vp, vp, i32, vp, vp, sz, vp]),
+            "arbor_truncate_scored": (ctypes.c_int, [G, T, Pl, vp, vp, vp, i32, vp, vp, vp, vp, sz,
+                                                     vp]),
             "arbor_fork": (ctypes.c_int, [G, T, Pl, vp, vp, vp, i32, vp, vp, vp, vp, sz, vp]),
             "arbor_append": (ctypes.c_int, [G, T, Pl, i32, ctypes.POINTER(Append), i32, vp, vp]),
             "arbor_prefill_plan_size": (sz, [G, i32, i32]),
@@ -160,7 +162,7 @@ def exported_symbols():
             "arbor_rehydrate", "arbor_tree_decode_attn",
             "arbor_tree_decode_attn_scored", "arbor_uncertainty",
             "arbor_uncertainty_workspace_size", "arbor_walk", "arbor_extend", "arbor_truncate",
-            "arbor_fork", "arbor_append", "arbor_prefill_plan_size", "arbor_prefill_plan",
+            "arbor_truncate_scored", "arbor_fork", "arbor_append", "arbor_prefill_plan_size", "arbor_prefill_plan",
             "arbor_prefill_workspace_size", "arbor_tree_prefill_attn"]
 
 
@@ -524,6 +526,23 @@ def arbor_truncate(kv: KVState, nodes, keep, status, workspace, stream=None) -> 
                                  _is(keep, "keep", torch.int32, (n,), dev), n,
                                  _is(status, "status", torch.int32, (1,), dev), ws, size,
                                  _stream_of(stream, dev))
+
+
+def arbor_truncate_scored(kv: KVState, nodes, keep, A, rows_seen, status, workspace,
+                          stream=None) -> int:
+    """arbor_truncate that also clears A of the tokens taken back, and rows_seen of blocks
+    left empty."""
+    dev, g, t, p, n_full = _descriptors(kv)
+    n = nodes.numel()
+    ws, size = _bytes(workspace, "workspace", dev)
+    return load().arbor_truncate_scored(g, t, p, n_full,
+                                        _is(nodes, "nodes", torch.int32, (n,), dev),
+                                        _is(keep, "keep", torch.int32, (n,), dev), n,
+                                        _is(A, "A", torch.float32, (kv.num_tokens,), dev),
+                                        _is(rows_seen, "rows_seen", torch.int64, (kv.num_nodes,),
+                                            dev),
+                                        _is(status, "status", torch.int32, (1,), dev), ws, size,
+                                        _stream_of(stream, dev))
 
 
 def arbor_fork(kv: KVState, src, dst, status, workspace, A=None, rows_seen=None,

@@ -33,8 +33,8 @@ int launch_extend(const arbor_geom_t *, arbor_tree_t *, arbor_pool_t *, int32_t 
                   int32_t, const int32_t *, int32_t, int64_t *, int32_t *, int64_t *, int32_t *,
                   void *, size_t, hipStream_t);
 int launch_truncate(const arbor_geom_t *, arbor_tree_t *, arbor_pool_t *, int32_t *,
-                    const int32_t *, const int32_t *, int32_t, int32_t *, void *, size_t,
-                    hipStream_t);
+                    const int32_t *, const int32_t *, int32_t, float *, int64_t *, int32_t *,
+                    void *, size_t, hipStream_t);
 int launch_fork(const arbor_geom_t *, arbor_tree_t *, arbor_pool_t *, int32_t *, const int32_t *,
                 const int32_t *, int32_t, float *, int64_t *, int32_t *, void *, size_t,
                 hipStream_t);
@@ -319,8 +319,18 @@ int arbor_truncate(const arbor_geom_t *geom, arbor_tree_t *tree, arbor_pool_t *p
                    int32_t *status, void *workspace, size_t workspace_bytes, hipStream_t stream) {
   ARBOR_TRY(check_grow(geom, tree, pool, n_full, n_nodes, status));
   if (n_nodes > 0 && (!nodes || !keep)) return ARBOR_EINVAL;
-  return launch_truncate(geom, tree, pool, n_full, nodes, keep, n_nodes, status, workspace,
-                         workspace_bytes, stream);
+  return launch_truncate(geom, tree, pool, n_full, nodes, keep, n_nodes, nullptr, nullptr, status,
+                         workspace, workspace_bytes, stream);
+}
+
+int arbor_truncate_scored(const arbor_geom_t *geom, arbor_tree_t *tree, arbor_pool_t *pool,
+                          int32_t *n_full, const int32_t *nodes, const int32_t *keep,
+                          int32_t n_nodes, float *A, int64_t *rows_seen, int32_t *status,
+                          void *workspace, size_t workspace_bytes, hipStream_t stream) {
+  ARBOR_TRY(check_grow(geom, tree, pool, n_full, n_nodes, status));
+  if (n_nodes > 0 && (!nodes || !keep || !A || !rows_seen)) return ARBOR_EINVAL;
+  return launch_truncate(geom, tree, pool, n_full, nodes, keep, n_nodes, A, rows_seen, status,
+                         workspace, workspace_bytes, stream);
 }
 
 int arbor_fork(const arbor_geom_t *geom, arbor_tree_t *tree, arbor_pool_t *pool,

@@ -9,7 +9,7 @@
 //             rows: slot, position and page-table entry of each new token;
 //   truncate  plan: the resident tokens each block keeps (a bounded search of
 //             its ascending slot positions), freed pages by a scan;
-//             clear: slot positions, page-table entries, pushed pages;
+//             clear: slot positions, page-table entries, pushed pages, A;
 //   fork      plan: pages by a scan; copy: K/V rows, slot positions, A.
 // Pages are popped and pushed in (node, page) order: page j of F popped is stack
 // entry top-1-j, and page j of F pushed becomes entry top+F-1-j, so that taking
@@ -220,7 +220,7 @@ __device__ int kept_below(const Tree &t, const Pool &pl, int i, int c, int n, in
 
 __global__ __launch_bounds__(kPlanThreads) void truncate_plan(
     Tree t, Pool pl, int32_t *n_full, const int32_t *__restrict__ nodes,
-    const int32_t *__restrict__ keep, int n_nodes, Grow g, int32_t *status) {
+    const int32_t *__restrict__ keep, int n_nodes, Grow g, int scored, int32_t *status) {
   __shared__ int64_t sm[2 * 16];
   if (status_failed(status)) {
     if (threadIdx.x == 0) g.meta[0] = 0;
@@ -239,7 +239,8 @@ __global__ __launch_bounds__(kPlanThreads) void truncate_plan(
       continue;
     }
     const int c = t.n_kept[i], n = t.n_full[i];
-    if (c < 0 || n < c || pages_of(c, P) > t.page_off[i + 1] - t.page_off[i]) {
+    if (c < 0 || n < c || pages_of(c, P) > t.page_off[i + 1] - t.page_off[i] ||
+        (scored && n > t.tok_off[i + 1] - t.tok_off[i])) {
       err = ARBOR_EINVAL;
       continue;
     }
@@ -280,10 +281,13 @@ __global__ __launch_bounds__(kPlanThreads) void truncate_plan(
 // (The plan takes 3.5 to 4.7 us, this launch 3.5 to 4.4, mostly their start and the latency of
 // five loads; the host does not know how many pages there are, so it is always made.)
 // 16 lanes a page: the slots from the first vacated one on, and, where the page is
-// freed, its table entry and its place on the stack.
+// freed, its table entry and its place on the stack.  With A, a workgroup a block: the
+// attention of the tokens taken back, and the rows that a block has seen once it is empty.
 __global__ __launch_bounds__(256) void truncate_clear(Tree t, Pool pl,
                                                       const int32_t *__restrict__ nodes,
-                                                      int n_nodes, Grow g, int32_t *status) {
+                                                      const int32_t *__restrict__ keep,
+                                                      int n_nodes, Grow g, float *A,
+                                                      int64_t *rows_seen, int32_t *status) {
   __shared__ int32_t sh_first[1024];
   const bool few = n_nodes <= 1024;
   if (few)
@@ -306,6 +310,13 @@ __global__ __launch_bounds__(256) void truncate_clear(Tree t, Pool pl,
       pl.free_stack[top + freed - 1 - (g.freed[e] + q - pages_of(left, P))] = page;
       t.page_table[at] = -1;
     }
+  }
+  if (!A) return;
+  for (int e = blockIdx.x; e < n_nodes; e += gridDim.x) {
+    const int i = nodes[e], n0 = g.n0[e], n1 = min(n0, keep[e]);
+    float *a = A + t.tok_off[i];
+    for (int p = n1 + threadIdx.x; p < n0; p += 256) a[p] = 0.0f;
+    if (threadIdx.x == 0 && n1 == 0) rows_seen[i] = 0;
   }
 }
 
@@ -464,16 +475,17 @@ int launch_extend(const arbor_geom_t *geom, arbor_tree_t *tree, arbor_pool_t *po
 
 int launch_truncate(const arbor_geom_t *geom, arbor_tree_t *tree, arbor_pool_t *pool,
                     int32_t *n_full, const int32_t *nodes, const int32_t *keep, int32_t n_nodes,
-                    int32_t *status, void *workspace, size_t workspace_bytes, hipStream_t stream) {
+                    float *A, int64_t *rows_seen, int32_t *status, void *workspace,
+                    size_t workspace_bytes, hipStream_t stream) {
   const Tree t = make_tree(tree);
   const Pool pl = make_pool(geom, pool);
   if (n_nodes == 0) return ARBOR_OK;
   Grow g;
   if (!carve(g, n_nodes, workspace, workspace_bytes)) return ARBOR_EWORKSPACE;
-  hipLaunchKernelGGL(truncate_plan, dim3(1), dim3(n_nodes <= 256 ? 256 : kPlanThreads), 0, stream, t, pl, n_full, nodes,
-                     keep, n_nodes, g, status);
-  hipLaunchKernelGGL(truncate_clear, dim3(128), dim3(256), 0, stream, t, pl, nodes, n_nodes, g,
-                     status);
+  hipLaunchKernelGGL(truncate_plan, dim3(1), dim3(n_nodes <= 256 ? 256 : kPlanThreads), 0, stream,
+                     t, pl, n_full, nodes, keep, n_nodes, g, A != nullptr, status);
+  hipLaunchKernelGGL(truncate_clear, dim3(128), dim3(256), 0, stream, t, pl, nodes, keep, n_nodes,
+                     g, A, rows_seen, status);
   return hip_ok(hipGetLastError());
 }
 
