@@ -533,7 +533,9 @@ size_t arbor_uncertainty_workspace_size(int32_t n_rows, int64_t vocab, int32_t d
  * arbor_truncate_scored has cleared.
  * Errors: EINVAL (ids, cu, a malformed tree, a block beyond its capacity, n_full
  * not tree->n_full), ENOPAGES, EUNSUPPORTED (a block deeper than
- * ARBOR_MAX_DEPTH), EWORKSPACE.
+ * ARBOR_MAX_DEPTH), EWORKSPACE, ECORRUPT (free_top outside [0, num_pages]; or a
+ * page outside the pool in the free stack or page table, which is found as its
+ * rows are written: such a pool was not consistent before, nor is it after).
  */
 int arbor_extend(const arbor_geom_t *geom, arbor_tree_t *tree, arbor_pool_t *pool,
                  int32_t *n_full, const int32_t *nodes, int32_t n_seq, const int32_t *cu,
@@ -584,7 +586,7 @@ int arbor_truncate_scored(const arbor_geom_t *geom, arbor_tree_t *tree, arbor_po
  * differ have different chains, so a copy means something below the same parent.
  * The token-span record is the caller's to copy (rows tok_off[src] + p).
  * Errors: EINVAL (ids, a dst that is not empty or too small, n_full not
- * tree->n_full), ENOPAGES, EWORKSPACE.
+ * tree->n_full), ENOPAGES, EWORKSPACE, ECORRUPT (as arbor_extend).
  */
 int arbor_fork(const arbor_geom_t *geom, arbor_tree_t *tree, arbor_pool_t *pool,
                int32_t *n_full, const int32_t *src, const int32_t *dst, int32_t n_forks, float *A,

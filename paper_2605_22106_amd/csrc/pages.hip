@@ -117,6 +117,7 @@ __global__ __launch_bounds__(kPlanThreads) void extend_plan(
   int64_t need = 0;
   const int top = *pl.free_top, oldest = n_seq > 0 ? nodes[0] : 0;
   if (threadIdx.x == 0 && (cu[0] != 0 || cu[n_seq] > n_tokens || cu[n_seq] < 0)) err = ARBOR_EINVAL;
+  if (top < 0 || top > pl.num_pages) err = ARBOR_ECORRUPT;      // (no stack to pop from)
   for (int e = r0; e < r1; ++e) {
     const int i = nodes[e], m = cu[e + 1] - cu[e];
     if (i < 0 || i >= t.V || (e > 0 && nodes[e - 1] >= i) || m < 0 || m > n_tokens) {
@@ -338,6 +339,7 @@ __global__ __launch_bounds__(kPlanThreads) void fork_plan(Tree t, Pool pl, int32
   const int top = *pl.free_top;
   for (int e = r0; e < r1; ++e) {
     const int a = src[e], b = dst[e];
+    if (top < 0 || top > pl.num_pages) err = ARBOR_ECORRUPT;
     if (a < 0 || a >= t.V || b < 0 || b >= t.V || (e > 0 && dst[e - 1] >= b)) {
       err = ARBOR_EINVAL;
       continue;

@@ -4,7 +4,7 @@ import pytest
 import torch
 
 from paper_2605_22106_amd import _lib as L
-from tests.gpu_helpers import check_rc, status, to_gpu
+from tests.gpu_helpers import check_rc, status, to_gpu, workspace
 from tests.grow_helpers import grow_state, ragged
 from tests.test_gpu_grow import append_case, split
 from tests.test_gpu_prefill import Prefill, queries
@@ -83,3 +83,21 @@ def test_a_block_with_more_tokens_than_pages(blocks):
         pf.status.zero_()
         pf(queries(kv, 4))                       # a plan that was refused is none
         assert int(pf.status) == L.EINVAL
+
+
+@pytest.mark.parametrize("top", [-1, 1, 1000])
+def test_a_stack_top_outside_the_stack(top):
+    """extend and fork pop no page from beyond the free stack."""
+    st = grow_state([-1, 0, 0, 0], [20, 33, 0, 0], kv_heads=1, layers=1, extra_pages=0)
+    kv = to_gpu(st)
+    kv.free_top.fill_(kv.num_pages + top if top > 0 else top)
+    before = [x.clone() for x in (kv.n_full, kv.n_kept, kv.page_table, kv.slot_pos, kv.free_top)]
+    i32 = lambda *x: torch.tensor(x, dtype=torch.int32, device="cuda")  # noqa: E731
+    slots, pos = torch.zeros(20, dtype=torch.int64, device="cuda"), i32(*[0] * 20)
+    for call in (lambda s: L.arbor_extend(kv, i32(1), i32(0, 20), slots, pos, None, s, workspace(kv)),
+                 lambda s: L.arbor_fork(kv, i32(1), i32(2), s, workspace(kv))):
+        s = status()
+        check_rc(call(s))
+        assert int(s) == L.ECORRUPT
+        for x, y in zip((kv.n_full, kv.n_kept, kv.page_table, kv.slot_pos, kv.free_top), before):
+            assert torch.equal(x, y)
