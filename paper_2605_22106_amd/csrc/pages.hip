@@ -346,7 +346,8 @@ __global__ __launch_bounds__(kPlanThreads) void fork_plan(Tree t, Pool pl, int32
     }
     const int c = t.n_kept[a], n = t.n_full[a];
     if (c < 0 || n < c || pages_of(c, P) > t.page_off[a + 1] - t.page_off[a] ||
-        t.n_kept[b] != 0 || t.n_full[b] != 0 || n > t.tok_off[b + 1] - t.tok_off[b] ||
+        n > t.tok_off[a + 1] - t.tok_off[a] || t.n_kept[b] != 0 || t.n_full[b] != 0 ||
+        n > t.tok_off[b + 1] - t.tok_off[b] ||
         pages_of(c, P) > t.page_off[b + 1] - t.page_off[b]) {
       err = ARBOR_EINVAL;
       continue;

@@ -101,3 +101,14 @@ def test_a_stack_top_outside_the_stack(top):
         assert int(s) == L.ECORRUPT
         for x, y in zip((kv.n_full, kv.n_kept, kv.page_table, kv.slot_pos, kv.free_top), before):
             assert torch.equal(x, y)
+
+
+def test_a_fork_of_more_tokens_than_the_capacity():
+    st = grow_state([-1, 0, 0], [20, 0, 60], spare=[40, 500, 0], kv_heads=1, layers=1)
+    kv = to_gpu(st)
+    kv.n_full[2] = 61                                 # the last block: its A would end beyond N
+    A = torch.ones(kv.num_tokens, device="cuda")
+    s = status()
+    one, two = (torch.tensor([x], dtype=torch.int32, device="cuda") for x in (1, 2))
+    check_rc(L.arbor_fork(kv, two, one, s, workspace(kv), A=A))
+    assert int(s) == L.EINVAL and int(kv.n_kept[1]) == 0 and bool((A == 1).all())
