@@ -282,7 +282,7 @@ __device__ bool merge_chains(const int32_t *n_kept, const O *page_off, int P, co
       const int64_t po = page_off[mine.node], end = page_off[mine.node + 1];
       mine.po = (int32_t)po;
       bad = bad || mine.limit < 0 || po < 0 || (end - po) * P < mine.limit;
-      need = (mine.limit + 15) / 16;
+      need = mine.limit / 16 + (mine.limit % 16 > 0);
     }
     const int inc = wave_inclusive_scan(need);
     mine.sub0 = subs + inc - need;
@@ -722,11 +722,10 @@ __device__ __forceinline__ float swap_halves_max(float v) {
 struct Window {
   int page;
   int info;      // first row of the page / 16 | valid rows << 8 | flags << 16
-  int place;     // chain block | first slot / 16 << 12
+  int ent;       // chain block
 };
 constexpr int kMask = 1 << 16;   // some row of this wave must not see some key of it
 constexpr int kNone = 1 << 17;   // no row of this wave sees any
-static_assert(kMaxSeq * MAXD <= 4096, "chain blocks of a tile fit 12 bits");
 
 // Whether the plan, whose header is h, is of this call and tree.
 __device__ __forceinline__ bool header_ok(const AttnArgs &a, const Header &h, int64_t table) {
@@ -839,7 +838,7 @@ __global__ __launch_bounds__(kRows * 2, 2) void prefill_attn(AttnArgs a) {
     const bool mask = mine != seqs || valid < 16 || (mown && slot + 15 > qmin);
     return Window{in && there ? page : 0,
                   slot % pl.P / 16 | valid << 8 | (none ? kNone : mask ? kMask : 0),
-                  at | slot / 16 << 12};
+                  at};
   };
 
   // the plane of this layer and head: pages are page_bytes apart
@@ -977,10 +976,9 @@ __global__ __launch_bounds__(kRows * 2, 2) void prefill_attn(AttnArgs a) {
 #pragma unroll
     for (int half = 0; half < 2; ++half) {
       const int idx = st % WSTEPS * C::SUBS + 2 * kt + half;
-      const int place = __builtin_amdgcn_readlane(cur.place, idx);
       const int valid = __builtin_amdgcn_readlane(cur.info, idx) >> 8 & 31;  // 0: past the end
-      const Entry en = entry(place & 4095);
-      const int slot = (place >> 12) * 16;
+      const Entry en = entry(__builtin_amdgcn_readlane(cur.ent, idx));
+      const int slot = (un.s0 + st * C::SUBS + 2 * kt + half - en.sub0) * 16;
       const int seen = en.own & seq_bit ? qslot + 1 - slot : en.below & seq_bit ? 16 : 0;
       const int lim = live ? min(seen, valid) : valid;
 #pragma unroll
