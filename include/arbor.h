@@ -665,8 +665,10 @@ int arbor_prefill_plan(const arbor_geom_t *geom, const arbor_tree_t *tree, const
  * reads of the ancestors that they have in common.  For bf16 pools the weights are
  * rounded to bf16 before their product with V (as V and the output are); all sums
  * are fp32.  What a token may not see (later tokens, other blocks, unused rows of a
- * page) has no influence on its output, infinities and NaN included.  Results are
- * bitwise reproducible.  Calls that run at once may share a plan, not a workspace.
+ * page) and the queries of others have no influence on its output, not on a bit of
+ * it, infinities and NaN included; how many tokens the call's blocks hold decides
+ * the order of its sums.  Results are bitwise reproducible.  Calls that run at once
+ * may share a plan, not a workspace.
  * `plan` is arbor_prefill_plan's for this n_seq and n_tokens; `workspace` holds
  * arbor_prefill_workspace_size() bytes.
  * Errors: EINVAL (arguments, a plan of another call or of a tree that has changed

@@ -927,13 +927,15 @@ __global__ __launch_bounds__(kRows * 2, 2) void prefill_attn(AttnArgs a) {
     t.sum = (part[0] + part[1]) + (part[2] + part[3]);
     return t;
   };
-  // the reference becomes at least the max of these logits, and what has been summed
-  // against the old one follows
-  auto raise = [&](const f32x16 &z) __attribute__((always_inline)) {
+  // the reference of the rows that move becomes at least the max of these logits, and what
+  // has been summed against the old one follows.  (Whether a row moves depends on the row
+  // alone, so that other rows of the wave do not change its bits.)
+  auto raise = [&](const f32x16 &z, bool moves) __attribute__((always_inline)) {
     float mx = z[0];
 #pragma unroll
     for (int x = 1; x < 16; ++x) mx = fmaxf(mx, z[x]);
-    const float to = fmaxf(ref, swap_halves_max(mx) * a.sl2);
+    mx = swap_halves_max(mx) * a.sl2;
+    const float to = moves ? fmaxf(ref, mx) : ref;
     if (ballot(to > ref)) {
       const float by = to == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(ref - to);
       l *= by;
@@ -969,6 +971,41 @@ __global__ __launch_bounds__(kRows * 2, 2) void prefill_attn(AttnArgs a) {
     }
   };
 
+  // term x of 16, as it goes into the products
+  auto weight = [&](const Terms &t, int x) __attribute__((always_inline)) -> float {
+    if constexpr (sizeof(T) == 2) return (float)t.p[x / 8][x % 8];
+    else return t.p[x];
+  };
+  // the same with 0 for values that are not finite
+  auto add_finite = [&](const Terms &t, int at, int kt) __attribute__((always_inline)) {
+    if constexpr (sizeof(T) == 2) {
+#pragma unroll
+      for (int ks = 0; ks < 2; ++ks)
+#pragma unroll
+        for (int d = 0; d < C::DT; ++d) {
+          u32x4 v = __builtin_bit_cast(u32x4, values(at, 2 * kt + ks, d));
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            if ((v[e] & 0x7f80u) == 0x7f80u) v[e] &= 0xffff0000u;
+            if ((v[e] & 0x7f800000u) == 0x7f800000u) v[e] &= 0xffffu;
+          }
+          o[d] = mfma_bf16(__builtin_bit_cast(bf16x8, v), t.p[ks], o[d]);
+          fence_order();                         // (one at a time, in few registers)
+        }
+    } else {
+#pragma unroll
+      for (int x = 0; x < 16; ++x)
+#pragma unroll
+        for (int d = 0; d < C::DT; ++d) {
+          const float v = *reinterpret_cast<const float *>(
+              lds + ((at + vat) ^ (d * C::STEP_V)) +
+              (2 * C::BUF + (8 * (x / 4) + x % 4) * C::ROW));
+          o[d] = mfma_f32(__builtin_isfinite(v) ? v : 0.0f, t.p[x], o[d]);
+          fence_order();
+        }
+    }
+  };
+
   // hides from each row the keys of half kt of step st that it may not see; the registers
   // hidden, for a careful run
   auto hide = [&](f32x16 &z, const Window &cur, int st, int kt) __attribute__((always_inline)) {
@@ -999,14 +1036,16 @@ __global__ __launch_bounds__(kRows * 2, 2) void prefill_attn(AttnArgs a) {
   // The new half's terms t of z against the reference, the reference raised where they
   // outgrow it.
   auto check = [&](Terms &t, const f32x16 &z) __attribute__((always_inline)) {
-    if (__builtin_expect(ballot(!(t.sum < kMoveAt)) != 0, 0)) {
+    const uint64_t over = ballot(!(t.sum < kMoveAt));
+    if (__builtin_expect(over != 0, 0)) {
       asm volatile("" ::: "memory");             // stays a branch: the rescale is long
-      raise(z);
+      raise(z, (over >> lr | over >> (lr + 32)) & 1);
       t = terms(z, base);
     }
     l += t.sum;
   };
-  // Any other step.  CAREFUL: see below.
+  // Any other step, bit by bit as a common one where a row has a reference.  CAREFUL: see
+  // below.
   auto plain_step = [&](const Window &cur, int st, int at, auto careful_c)
                         __attribute__((always_inline)) {
     constexpr bool CAREFUL = decltype(careful_c)::value;
@@ -1020,7 +1059,7 @@ __global__ __launch_bounds__(kRows * 2, 2) void prefill_attn(AttnArgs a) {
           hidden = hide(z, cur, st, kt);
           masked = __builtin_amdgcn_readfirstlane(1);
         }
-        raise(z);
+        raise(z, ref == -INFINITY);
         all_set = __builtin_amdgcn_readfirstlane(ballot(ref == -INFINITY) == 0);
       }
       Terms t = terms(z, base);
@@ -1028,16 +1067,18 @@ __global__ __launch_bounds__(kRows * 2, 2) void prefill_attn(AttnArgs a) {
       if (!CAREFUL || !mask) {
         add(t, at, kt);
       } else if constexpr (CAREFUL) {
-        // 16 keys of P at a time go through the buffer that a careful run does not load
-        // into; a hidden key is marked by -1
+        // The products with every value that is finite, as always: the bits of rows that
+        // see no others do not change.  Then the others, for the rows that see them: 16 keys
+        // of P at a time go through the buffer that a careful run does not load into; a
+        // hidden key is marked by -1
+        add_finite(t, at, kt);
         float *scr = reinterpret_cast<float *>(lds + C::BUF) + wave * 512;
 #pragma unroll
         for (int ks = 0; ks < 2; ++ks) {
 #pragma unroll
           for (int e = 0; e < 8; ++e)
             scr[(8 * (e / 4) + 4 * h + e % 4) * 32 + lr] =
-                hidden >> (8 * ks + e) & 1
-                    ? -1.0f : __builtin_amdgcn_exp2f(__builtin_fmaf(z[8 * ks + e], a.sl2, -base));
+                hidden >> (8 * ks + e) & 1 ? -1.0f : weight(t, 8 * ks + e);
           __builtin_amdgcn_s_waitcnt(0);
           __builtin_amdgcn_wave_barrier();
           for (int key = 0; key < 16; ++key) {
@@ -1047,10 +1088,11 @@ __global__ __launch_bounds__(kRows * 2, 2) void prefill_attn(AttnArgs a) {
             for (int d = 0; d < C::DT; ++d)
 #pragma unroll
               for (int x = 0; x < 16; ++x) {
+                if (x % 4 == 0) fence_order();
                 const int c = 32 * d + 8 * (x / 4) + 4 * h + x % 4;
                 const float vv = (float)*reinterpret_cast<const T *>(
                     vr + v_piece<T, D>(key, c * C::ES / 16) * 16 + c * C::ES % 16);
-                o[d][x] = pk < 0.0f ? o[d][x] : o[d][x] + pk * vv;
+                o[d][x] = pk < 0.0f || __builtin_isfinite(vv) ? o[d][x] : o[d][x] + pk * vv;
               }
           }
           __builtin_amdgcn_wave_barrier();
@@ -1133,7 +1175,7 @@ __global__ __launch_bounds__(kRows * 2, 2) void prefill_attn(AttnArgs a) {
   }
   // A key that a row may not see has p = 0, but 0 times an infinite or NaN value is not
   // 0.  So a unit that hid keys and whose outputs are not all finite runs once more, its
-  // steps with hidden keys summed key by key, without them.
+  // steps with hidden keys without such values but for the rows that see them.
   float odd = 0.0f;                            // NaN if some output is not finite
   if (masked)
 #pragma unroll
