@@ -115,12 +115,17 @@ __host__ __device__ inline int target_parts(int Hkv) {
   return t > 0 ? t : 1;
 }
 
-// Whether the plan may cut a tile.  Of one block with twice as many tiles as the chip holds
-// for a KV head, none has more than about twice the average's keys, so none would be: the
-// call goes without the second launch (6 us a layer of 164, 4,096 tokens of the 8B shape).
-inline bool may_split(const arbor_geom_t *g, int n_seq, int n_tokens) {
-  return n_seq > 1 ||
-         n_tokens / tokens_per_tile(g->q_per_kv) < 2 * target_parts(g->num_kv_heads);
+// Workgroups of the join.  Of one block with twice as many tiles as the chip holds for a KV
+// head, none has more than about twice the average's keys, so none is cut, unless most of
+// the packed rows are padding, which only the device knows: a few workgroups see to that,
+// one item after the other (2 us a layer of 160 where there is none, 4,096 tokens of the 8B
+// shape; with as many as elsewhere 6).
+inline int64_t join_groups(const arbor_geom_t *g, int n_seq, int n_tokens, int64_t tiles) {
+  const int target = target_parts(g->num_kv_heads);
+  const int64_t cut = tiles < target / 2 ? tiles : target / 2;     // (two parts or more each)
+  const int64_t all = cut * g->num_kv_heads * kWaves;
+  const bool whole = n_seq == 1 && n_tokens / tokens_per_tile(g->q_per_kv) >= 2 * target;
+  return whole && all > 256 ? 256 : all;
 }
 
 PlanPtrs carve_plan(const arbor_geom_t *g, int n_seq, int n_tokens, void *plan, size_t bytes,
@@ -1255,79 +1260,80 @@ template <class T, int D>
 __global__ __launch_bounds__(256) void prefill_join(AttnArgs a) {
   constexpr int U = 4, QUADS = D / 8;
   const Pool &pl = a.pl;
-  int x = blockIdx.x;
-  const int rows = x % kWaves;                  // 32 rows: the wave that had them
-  x /= kWaves;
-  const int g = x % pl.Hkv, k = x / pl.Hkv;
+  const int per_tile = kWaves * pl.Hkv;
   const int32_t status = status_word(a.status);
   Header head_of = *a.p.head;
   const int64_t table = a.t.page_off[a.t.V];
-  int4 tl = a.p.split[min(k, target_parts(pl.Hkv) - 1)];
+  int4 tl = a.p.split[min((int)blockIdx.x / per_tile, target_parts(pl.Hkv) - 1)];
   asm volatile("" : "+s"(head_of.n_split), "+s"(tl.x), "+s"(tl.y), "+s"(tl.z), "+s"(tl.w));
-  if (!header_ok(a, head_of, table) | (k >= head_of.n_split)) return;
-  if (status < 0) return;
-  const int t0 = tl.x, nt = tl.y, part0 = tl.z, parts = tl.w;
-  if (rows * 32 / pl.G >= nt || part0 + parts > a.part_cap) return;
-  const int lane = lane_id(), wave = threadIdx.x / kWave, lr = lane & 31, h = lane >> 5;
-  const int64_t stride = (int64_t)pl.Hkv * kWaves * part_floats<D>();
-  const float *pp = a.part + (((int64_t)part0 * pl.Hkv + g) * kWaves + rows) * part_floats<D>();
-  constexpr int MINE = QUADS / 4;               // quads of a wave
-  f32x4 o[MINE], v[U][MINE];
-  float ref[U], sum[U];
-  auto load = [&](int e0) {
+  if (!header_ok(a, head_of, table) | (status < 0)) return;
+  for (int x = blockIdx.x; x / per_tile < head_of.n_split; x += gridDim.x) {
+    if (x != (int)blockIdx.x) tl = a.p.split[x / per_tile];
+    const int rows = x % kWaves;                  // 32 rows: the wave that had them
+    const int g = x / kWaves % pl.Hkv;
+    const int t0 = tl.x, nt = tl.y, part0 = tl.z, parts = tl.w;
+    if (rows * 32 / pl.G >= nt || part0 + parts > a.part_cap) continue;
+    const int lane = lane_id(), wave = threadIdx.x / kWave, lr = lane & 31, h = lane >> 5;
+    const int64_t stride = (int64_t)pl.Hkv * kWaves * part_floats<D>();
+    const float *pp = a.part + (((int64_t)part0 * pl.Hkv + g) * kWaves + rows) * part_floats<D>();
+    constexpr int MINE = QUADS / 4;               // quads of a wave
+    f32x4 o[MINE], v[U][MINE];
+    float ref[U], sum[U];
+    auto load = [&](int e0) {
 #pragma unroll
-    for (int i = 0; i < U; ++i) {
-      ref[i] = -INFINITY;
-      if (e0 + i >= parts) continue;
-      const float *q = pp + (e0 + i) * stride;
-      ref[i] = q[32 * D + lr];
-      sum[i] = q[32 * D + 32 + lr];
+      for (int i = 0; i < U; ++i) {
+        ref[i] = -INFINITY;
+        if (e0 + i >= parts) continue;
+        const float *q = pp + (e0 + i) * stride;
+        ref[i] = q[32 * D + lr];
+        sum[i] = q[32 * D + 32 + lr];
 #pragma unroll
-      for (int j = 0; j < MINE; ++j)
-        v[i][j] = *reinterpret_cast<const f32x4 *>(q + ((wave * MINE + j) * kWave + lane) * 4);
-    }
-  };
-  float m = -INFINITY, l = 0.0f;
-#pragma unroll
-  for (int j = 0; j < MINE; ++j) o[j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-  for (int e0 = 0; e0 < parts; e0 += U) {
-    load(e0);
-    float to = m;
-#pragma unroll
-    for (int i = 0; i < U; ++i) to = fmaxf(to, ref[i]);
-    const float base = to == -INFINITY ? 0.0f : to;
-    const float by = m == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m - base);
-    l *= by;
-#pragma unroll
-    for (int j = 0; j < MINE; ++j) o[j] *= by;
-    m = to;
-#pragma unroll
-    for (int i = 0; i < U; ++i)
-      if (e0 + i < parts) {
-        // a part whose terms have no reference holds sums of 0 (or NaN, which stays)
-        const float w = ref[i] == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(ref[i] - base);
-        l += w * sum[i];
-#pragma unroll
-        for (int j = 0; j < MINE; ++j) o[j] += w * v[i][j];
+        for (int j = 0; j < MINE; ++j)
+          v[i][j] = *reinterpret_cast<const f32x4 *>(q + ((wave * MINE + j) * kWave + lane) * 4);
       }
-  }
-  const int row = rows * 32 + lr, tq = row / pl.G;
-  if (tq >= nt) return;
-  const float inv = l == 0.0f ? 0.0f : 1.0f / l;
-  const int Hq = pl.Hkv * pl.G, head = g * pl.G + row - tq * pl.G;
-  const int64_t tok = t0 + tq;
-  typedef T ovec __attribute__((ext_vector_type(4)));
+    };
+    float m = -INFINITY, l = 0.0f;
 #pragma unroll
-  for (int j = 0; j < MINE; ++j) {
-    ovec w;
+    for (int j = 0; j < MINE; ++j) o[j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    for (int e0 = 0; e0 < parts; e0 += U) {
+      load(e0);
+      float to = m;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) w[i] = (T)(o[j][i] * inv);
-    *reinterpret_cast<ovec *>(static_cast<T *>(a.out) + (tok * Hq + head) * D +
-                              (wave * MINE + j) * 8 + 4 * h) = w;
+      for (int i = 0; i < U; ++i) to = fmaxf(to, ref[i]);
+      const float base = to == -INFINITY ? 0.0f : to;
+      const float by = m == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m - base);
+      l *= by;
+#pragma unroll
+      for (int j = 0; j < MINE; ++j) o[j] *= by;
+      m = to;
+#pragma unroll
+      for (int i = 0; i < U; ++i)
+        if (e0 + i < parts) {
+          // a part whose terms have no reference holds sums of 0 (or NaN, which stays)
+          const float w = ref[i] == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(ref[i] - base);
+          l += w * sum[i];
+#pragma unroll
+          for (int j = 0; j < MINE; ++j) o[j] += w * v[i][j];
+        }
+    }
+    const int row = rows * 32 + lr, tq = row / pl.G;
+    if (tq >= nt) continue;
+    const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+    const int Hq = pl.Hkv * pl.G, head = g * pl.G + row - tq * pl.G;
+    const int64_t tok = t0 + tq;
+    typedef T ovec __attribute__((ext_vector_type(4)));
+#pragma unroll
+    for (int j = 0; j < MINE; ++j) {
+      ovec w;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) w[i] = (T)(o[j][i] * inv);
+      *reinterpret_cast<ovec *>(static_cast<T *>(a.out) + (tok * Hq + head) * D +
+                                (wave * MINE + j) * 8 + 4 * h) = w;
+    }
+    if (a.lse && wave == 0 && h == 0)
+      a.lse[tok * Hq + head] = ((m == -INFINITY && l != 0.0f ? 0.0f : m) +
+                                __builtin_amdgcn_logf(l)) * kLn2;
   }
-  if (a.lse && wave == 0 && h == 0)
-    a.lse[tok * Hq + head] = ((m == -INFINITY && l != 0.0f ? 0.0f : m) +
-                              __builtin_amdgcn_logf(l)) * kLn2;
 }
 
 inline size_t tile_floats(const arbor_geom_t *g) {      // of a part, all KV heads
@@ -1355,8 +1361,7 @@ int launch_prefill_plan(const arbor_geom_t *geom, const arbor_tree_t *tree, cons
   const Tree t = make_tree(tree);
   const int G = geom->q_per_kv, Hkv = geom->num_kv_heads, P = geom->page_size;
   const int target = target_parts(Hkv);
-  const int min_part = may_split(geom, n_seq, n_tokens)
-                           ? kMinSteps * step_subs(geom->dtype == ARBOR_BF16 ? 2 : 4) : INT32_MAX;
+  const int min_part = kMinSteps * step_subs(geom->dtype == ARBOR_BF16 ? 2 : 4);
   if (n_seq <= kMaxSeq && p.tiles_cap <= kSmallTiles && t.V <= kSmallV) {
     hipLaunchKernelGGL(plan_small, dim3(1), dim3(1024), 0, stream, t, G, Hkv, P, nodes, n_seq, cu,
                        n_tokens, p, target, min_part, status);
@@ -1393,11 +1398,8 @@ int launch_prefill(const arbor_geom_t *geom, const arbor_tree_t *tree, const arb
   a.lse = lse;
   a.sl2 = (softmax_scale > 0.0f ? softmax_scale : 1.0f / sqrtf((float)geom->head_dim)) * kLog2e;
   a.status = status;
-  const int target = target_parts(geom->num_kv_heads);
   const int64_t units = a.p.units_cap * geom->num_kv_heads;
-  // tiles of two parts or more
-  const int64_t split = !may_split(geom, n_seq, n_tokens) ? 0
-                        : a.p.tiles_cap < target / 2 ? a.p.tiles_cap : target / 2;
+  const int64_t joins = join_groups(geom, n_seq, n_tokens, a.p.tiles_cap);
   if (units > INT32_MAX) return ARBOR_EUNSUPPORTED;
 #define ARBOR_PREFILL_LAUNCH(T, D)                                                             \
   do {                                                                                         \
@@ -1405,10 +1407,8 @@ int launch_prefill(const arbor_geom_t *geom, const arbor_tree_t *tree, const arb
     hipLaunchKernelGGL((prefill_attn<T, D>), dim3((unsigned)units), dim3(kRows * 2),           \
                        (Cfg<T, D>::LDS), stream, a);                                           \
     timing_end(geom, ARBOR_KERNEL_PREFILL_ATTN, stream);                                       \
-    if (split > 0)                                                                             \
-      hipLaunchKernelGGL((prefill_join<T, D>),                                                 \
-                         dim3((unsigned)(split * geom->num_kv_heads * kWaves)),                \
-                         dim3(256), 0, stream, a);                                             \
+    if (joins > 0)                                                                             \
+      hipLaunchKernelGGL((prefill_join<T, D>), dim3((unsigned)joins), dim3(256), 0, stream, a); \
   } while (0)
   if (geom->dtype == ARBOR_BF16) {
     if (geom->head_dim == 128) ARBOR_PREFILL_LAUNCH(__bf16, 128);
