@@ -218,6 +218,9 @@ class KVState:
         self.__dict__.pop("_built", None)       # see _descriptors
         self.__dict__[name] = value
 
+    def __getstate__(self):                     # copies and pickles build their own
+        return {k: v for k, v in self.__dict__.items() if k != "_built"}
+
     @property
     def num_nodes(self) -> int:
         return int(self.parent.numel())
