@@ -473,7 +473,10 @@ def _descriptors(kv: KVState):
     d = kv.__dict__.get("_built")
     if d is None or d[0] != now:
         g, t, p = kv.geom(), kv.tree(), kv.pool()
-        d = (now, kv.k.get_device(), ctypes.byref(g), ctypes.byref(t), ctypes.byref(p))
+        device = kv.k.get_device()
+        if any(x.get_device() != device for x in vars(kv).values() if isinstance(x, torch.Tensor)):
+            raise ValueError("the tree and pool must be on one device")
+        d = (now, device, ctypes.byref(g), ctypes.byref(t), ctypes.byref(p))
         kv.__dict__["_built"] = d
     if d[1] != torch.cuda.current_device():
         raise ValueError("the tree and pool must be on the current device")

@@ -1,4 +1,5 @@
-"""A KVState that has been used in a call is copied, pickled and saved as one that has not."""
+"""A KVState that has been used in a call is copied, pickled and saved as one that has not, and
+lies on one device."""
 import copy
 import dataclasses
 import io
@@ -38,3 +39,16 @@ def test_copies_of_a_used_state(used, make):
     g, t = L._descriptors(new)[1:3]
     assert t._obj.parent == new.parent.data_ptr() and g._obj.num_pages == 9
     assert L._descriptors(used)[2]._obj.parent == used.parent.data_ptr()
+
+
+def test_a_state_on_two_devices_is_refused(used):
+    class Elsewhere(torch.Tensor):
+        def get_device(self):
+            return 1
+    for name in ("parent", "page_table", "v", "free_top"):
+        here = getattr(used, name)
+        setattr(used, name, here.as_subclass(Elsewhere))
+        with pytest.raises(ValueError, match="one device"):
+            L._descriptors(used)
+        setattr(used, name, here)
+    L._descriptors(used)
