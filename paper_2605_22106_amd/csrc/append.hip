@@ -328,10 +328,11 @@ __global__ __launch_bounds__(256) void append_rows(AppendArgs args) {
   }
 }
 
-// The same with eight elements in a row a lane; see above.  A step's registers take the
-// next load as soon as they are read; where a wave takes a token by itself two in flight,
-// with the sines read from LDS, leave eight waves to a SIMD (six: 87 us and more).  Each
-// line is read once and written once, past the caches (7 us more with ordinary stores).
+// The same with eight elements in a row a lane; see above.  A workgroup of four waves, or of
+// one, takes a token.  A step's registers take the next load as soon as they are read, two
+// steps ahead (four: as fast in the 70B shape, 5 to 15 % slower in fp32 and for fewer
+// heads).  Each line is read once and written once, past the caches (with ordinary stores
+// 8,192 tokens of the 8B shape 48 us against 45, of the 70B shape 82 against 74).
 // 8,192 tokens of 64 + 8 + 8 heads of 128 bf16, 336 MB: 70 us, 4.8 TB/s of the 5.1 of a
 // large copy.
 //
@@ -344,7 +345,7 @@ __global__ __launch_bounds__(BLOCK, BLOCK == 64 && sizeof(T) == 2 ? 8 : 4) void 
     AppendArgs args) {
   constexpr int LPR = D / 8;                    // lanes of a head
   constexpr int RPS = BLOCK / LPR;              // heads a step
-  constexpr int UNROLL = BLOCK == 64 ? 2 : 4;   // steps whose loads are in flight together
+  constexpr int UNROLL = 2;                     // steps whose loads are in flight together
   constexpr int W = sizeof(T) * 2;              // words of eight elements
   struct Eight {
     T e[8];
@@ -487,10 +488,20 @@ __global__ __launch_bounds__(BLOCK, BLOCK == 64 && sizeof(T) == 2 ? 8 : 4) void 
   }
 }
 
-// From here on a wave takes a token by itself: 256 CUs hold as many waves at eight a SIMD.
-// The 70B shape, one wave and four: 2,048 tokens 41 and 27 us, 4,096 54 and 45, 8,192 76 and
-// 85, 16,384 148 and 164.
-constexpr int kManyTokens = 8192;
+// Whether a wave takes a token by itself.  Four waves have a token's heads in flight at
+// once, one wave takes them a few at a time but wastes no lanes, and forms the sines once in
+// as many waves: it wins where tokens are many and their heads few.  In lanes of a token's
+// heads (16 a head of 128, 8 a head of 64), one wave and four, us: 48 lanes, 1,000 tokens 3.8
+// and 4.2, 16,384 12.9 and 20.4; 128 lanes, 1,000 4.9 and 4.5, 2,000 5.9 and 6.0, 16,384 19
+// and 27; 256 lanes, 2,000 8.0 and 7.0, 4,000 11.4 and 11.5, 16,384 29 and 38; 512 lanes,
+// 4,000 19.1 and 17.5, 8,192 30.2 and 31.7; 768 lanes, 8,192 45.0 and 45.2, 16,384 88.5 and
+// 88.2; 1,280 lanes, 8,192 78 and 73, 16,384 152 and 151.  fp32: 128 lanes, 1,000 4.4 and
+// 4.4, 16,384 30 and 39; 256 lanes, 1,000 6.7 and 5.5, 4,000 16.4 and 17.0, 16,384 58 and 61;
+// 384 lanes, 8,192 46 and 42, 16,384 89 and 82.
+inline bool wave_a_token(const arbor_geom_t *g, int n_tokens) {
+  const int64_t lanes = (int64_t)g->num_kv_heads * (g->q_per_kv + 2) * (g->head_dim / 8);
+  return n_tokens >= 16 * lanes && lanes <= (g->dtype == ARBOR_BF16 ? 512 : 256);
+}
 
 }  // namespace
 
@@ -499,7 +510,7 @@ int launch_append(const arbor_geom_t *geom, const arbor_tree_t *tree, arbor_pool
                   hipStream_t stream) {
   if (n_tokens == 0) return ARBOR_OK;
   const AppendArgs args{make_pool(geom, pool), *a, tree->num_tokens, layer, n_tokens, status};
-  const bool many = n_tokens >= kManyTokens;
+  const bool many = wave_a_token(geom, n_tokens);
 #define ARBOR_APPEND_WHOLE(T, D, HALVES)                                                         \
   do {                                                                                           \
     if (many)                                                                                    \

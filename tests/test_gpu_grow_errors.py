@@ -12,7 +12,7 @@ from tests.test_gpu_prefill import Prefill, queries
 pytestmark = pytest.mark.gpu
 
 
-@pytest.mark.parametrize("tokens,rotary,record", [(5000, 128, False), (9000, 128, True),
+@pytest.mark.parametrize("tokens,rotary,record", [(2900, 128, False), (9000, 128, True),
                                                   (5000, 64, True), (5000, 0, False)])
 def test_a_bad_slot_leaves_other_tokens_whole(tokens, rotary, record):
     """The token with the bad slot is left out; each other token is written whole, queries, keys,
