@@ -463,9 +463,12 @@ int launch_extend(const arbor_geom_t *geom, arbor_tree_t *tree, arbor_pool_t *po
   if (!carve(g, n_seq, workspace, workspace_bytes)) return ARBOR_EWORKSPACE;
   // up to 4,096 tokens the plan's workgroup writes their rows itself
   const int rows_too = n_tokens <= 4 * kPlanThreads;
-  // few waves meet at a barrier sooner (48 blocks, 288 tokens: 6.6 us, 7.1 with 1,024
-  // threads), but a thread that has two tokens waits twice (496: 8.0, 7.4)
-  const int threads = n_seq <= 256 && n_tokens <= 320 ? 256 : kPlanThreads;
+  // Few waves meet at a barrier sooner, but a thread that has two tokens waits twice: the
+  // smallest group with a thread for each token and block.  (A truncate and an extend of 48
+  // blocks with 256, 512 and 1,024 threads, us: 200 tokens 13.8, 13.8, 14.1; 288 tokens
+  // 15.1, 14.0, 14.3; 640 tokens 16.4, 15.2, 14.6.)
+  const int most = n_seq > n_tokens ? n_seq : n_tokens;
+  const int threads = most <= 256 ? 256 : most <= 512 ? 512 : kPlanThreads;
   hipLaunchKernelGGL(extend_plan, dim3(1), dim3(threads), 0, stream, t, pl, n_full, nodes,
                      n_seq, cu, n_tokens, g, slots, positions, tokens, rows_too, status);
   if (!rows_too) {
