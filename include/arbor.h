@@ -511,7 +511,8 @@ size_t arbor_uncertainty_workspace_size(int32_t n_rows, int64_t vocab, int32_t d
  * (e < n_seq, device int32, strictly ascending ids) gets the tokens cu[e] ..
  * cu[e+1]-1 of the packed rows (cu: device int32 [n_seq+1], cu[0] = 0, not
  * descending; a block may get none).  n_tokens rows are packed in all; rows from
- * cu[n_seq] on are padding, which every call leaves as it was.  A step of a
+ * cu[n_seq] on are padding: arbor_extend marks them in its outputs, and the calls
+ * that follow leave their rows of the outputs as they were.  A step of a
  * model is one arbor_extend, one arbor_prefill_plan, and for each layer
  * arbor_append and arbor_tree_prefill_attn (or arbor_tree_decode_attn where
  * every block got one token).

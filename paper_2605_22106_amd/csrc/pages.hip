@@ -50,7 +50,8 @@ __device__ __forceinline__ int last_at_most(const T *first, int n, T x) {
 }
 
 // Tokens that the block x gets in this call (0 unless it is listed).
-__device__ __forceinline__ int listed_tokens(const int32_t *nodes, const int32_t *cu, int n, int x) {
+__device__ __forceinline__ int listed_tokens(const int32_t *nodes, const int32_t *cu, int n,
+                                             int x) {
   const int e = last_at_most(nodes, n, x);
   return nodes[e] == x ? cu[e + 1] - cu[e] : 0;
 }
@@ -90,9 +91,9 @@ __device__ void extend_rows(const Tree &t, const Pool &pl, const int32_t *__rest
   }
 }
 
-// Latency: checks 1.3 us, a vote 0.5, walks 1.1, scan 0.8, rows 1.5 (6.6 us for 48 blocks and
-// 288 tokens, 7.4 for 16 blocks four levels down and 496 tokens; walks in memory, a dependent
-// load a level: 7.9).
+// Latency: checks 1.3 us, a vote 0.5, walks 1.1, scan 0.8, rows 1.5 (6.9 us for 48 blocks and
+// 175 tokens, 7.4 for 16 blocks four levels down and 496 tokens; walks in memory, a dependent
+// load a level: 0.5 more).
 __global__ __launch_bounds__(kPlanThreads) void extend_plan(
     Tree t, Pool pl, int32_t *n_full, const int32_t *__restrict__ nodes, int n_seq,
     const int32_t *__restrict__ cu, int n_tokens, Grow g, int64_t *__restrict__ slots,
@@ -436,6 +437,11 @@ __global__ __launch_bounds__(256) void fork_copy(Tree t, Pool pl, const int32_t 
   }
 }
 
+// Threads of the plans of truncate and fork: a fork and a truncate of 4 blocks with 256 and
+// 1,024 threads 13.6 and 14.5 us, of 48 15.4 and 16.4, of 256 16.8 and 17.7; of more a thread
+// would take several.
+inline int plan_threads(int n) { return n <= 256 ? 256 : kPlanThreads; }
+
 bool carve(Grow &g, int n, void *workspace, size_t bytes) {
   Carve cv(workspace, bytes);
   g.c0 = cv.take<int32_t>(n);
@@ -488,8 +494,8 @@ int launch_truncate(const arbor_geom_t *geom, arbor_tree_t *tree, arbor_pool_t *
   if (n_nodes == 0) return ARBOR_OK;
   Grow g;
   if (!carve(g, n_nodes, workspace, workspace_bytes)) return ARBOR_EWORKSPACE;
-  hipLaunchKernelGGL(truncate_plan, dim3(1), dim3(n_nodes <= 256 ? 256 : kPlanThreads), 0, stream,
-                     t, pl, n_full, nodes, keep, n_nodes, g, A != nullptr, status);
+  hipLaunchKernelGGL(truncate_plan, dim3(1), dim3(plan_threads(n_nodes)), 0, stream, t, pl,
+                     n_full, nodes, keep, n_nodes, g, A != nullptr, status);
   hipLaunchKernelGGL(truncate_clear, dim3(128), dim3(256), 0, stream, t, pl, nodes, keep, n_nodes,
                      g, A, rows_seen, status);
   return hip_ok(hipGetLastError());
@@ -504,12 +510,12 @@ int launch_fork(const arbor_geom_t *geom, arbor_tree_t *tree, arbor_pool_t *pool
   if (n_forks == 0) return ARBOR_OK;
   Grow g;
   if (!carve(g, n_forks, workspace, workspace_bytes)) return ARBOR_EWORKSPACE;
-  hipLaunchKernelGGL(fork_plan, dim3(1), dim3(n_forks <= 256 ? 256 : kPlanThreads), 0, stream, t, pl, n_full, src, dst,
-                     n_forks, g, rows_seen, status);
+  hipLaunchKernelGGL(fork_plan, dim3(1), dim3(plan_threads(n_forks)), 0, stream, t, pl, n_full,
+                     src, dst, n_forks, g, rows_seen, status);
   const int copies = 2048;
   const int marks = A ? (n_forks < 256 ? n_forks : 256) : 0;
-  hipLaunchKernelGGL(fork_copy, dim3(copies + marks), dim3(256), 0, stream, t, pl, src, dst, n_forks,
-                     g, A, copies, status);
+  hipLaunchKernelGGL(fork_copy, dim3(copies + marks), dim3(256), 0, stream, t, pl, src, dst,
+                     n_forks, g, A, copies, status);
   return hip_ok(hipGetLastError());
 }
 

@@ -22,13 +22,16 @@
 // through a buffer resource over the valid rows of a sub-page, which fills the
 // others with zeros; those of the next step are issued before this step's products.
 //
-// What bounds it: LDS.  A step of 64 keys reads 16 KB of K and 16 KB of V from LDS in
-// each of four waves, for 4 MFLOP of products a wave, and 32 KB arrive.  8,192 tokens of
-// the 70B shape (1.1 TFLOP): 1.07 ms, 1.03 PFLOP/s (a library's 8,192^3 product: 1.3 to
-// 1.5); with the reads of K left out 0.88 ms, of V 1.07, of both 0.80, without the loads
-// 0.97, with none of these 0.64.  64 rows a wave halve the reads, but leave one wave to a
-// SIMD, which ran 1.55 ms and more; 32 keys a step and three waves 1.77.  fp32: 122
-// TFLOP/s of the 153 of a library's product.
+// What bounds it: the matrix and vector work of two waves a SIMD, each a chain of logits,
+// exponentials and products, which overlap in part.  A step of 64 keys is 1.05 MFLOP of
+// products a wave; 8,192 tokens of the 70B shape (1.1 TFLOP) take 1.07 ms, 1.03 PFLOP/s (a
+// library's 8,192^3 product: 1.3 to 1.5), of which the matrix units are busy for 50 %; a wave
+// waits for its unit in 34 % of its cycles and for data in 25 %.  The same without data
+// movement takes 0.88 ms; left out one by one, the loads to LDS are 0.12 ms, the reads of K
+// 0.05, of V, which are three products ahead, 0.02.  64 rows a wave halve the reads, but
+// leave one wave to a SIMD, which ran 1.55 ms and more; 32 keys a step and three waves 1.77.
+// fp32, 4,096 tokens: 132 TFLOP/s in the 70B shape, 115 in the 8B shape, of the 153 of a
+// library's product.
 #include <type_traits>
 
 #include "arbor_internal.h"
@@ -487,16 +490,20 @@ __global__ __launch_bounds__(1024) void plan_small(Tree t, int G, int Hkv, int P
   __shared__ int32_t sh_parent[kSmallV], sh_kept[kSmallV], sh_page_off[kSmallV + 1];
   __shared__ uint16_t chain[MAXD * kCol];
   __shared__ Tile tiles[kSmallTiles];
-  __shared__ int n_tiles;
+  __shared__ int n_tiles, bad;
   const int wave = threadIdx.x >> 6, lane = lane_id();
   const int leaf = wave == 1 && lane < n_seq ? nodes[lane] : -1;
-  for (int i = threadIdx.x; i < t.V; i += 1024) {
-    sh_parent[i] = t.parent[i];
-    sh_kept[i] = t.n_kept[i];
+  for (int i = threadIdx.x; i <= t.V; i += 1024) {
+    const int j = min(i, t.V - 1);                 // (no branch: all loads are in flight together)
+    const int up = t.parent[j], kept = t.n_kept[j];
     sh_page_off[i] = (int32_t)t.page_off[i];
+    sh_parent[j] = up;
+    sh_kept[j] = kept;
   }
-  if (threadIdx.x == 0) sh_page_off[t.V] = (int32_t)t.page_off[t.V];
-  if (threadIdx.x == 0) p.head->magic = 0;
+  if (threadIdx.x == 0) {
+    p.head->magic = 0;
+    bad = 0;
+  }
   if (status_failed(status)) return;
   if (!request_ok(t, nodes, n_seq, cu, n_tokens, sh_cu)) {
     if (threadIdx.x == 0) status_error(status, ARBOR_EINVAL);
@@ -517,12 +524,14 @@ __global__ __launch_bounds__(1024) void plan_small(Tree t, int G, int Hkv, int P
   }
   for (int k = wave; k < n_tiles; k += 16) {
     const int col = min(tiles[k].e0 + lane, kWave - 1);
-    if (!merge_chains(sh_kept, sh_page_off, P, sh_cu, p, k, &tiles[k], chain, col, depth[col]))
-      err = ARBOR_EINVAL;
+    if (!merge_chains(sh_kept, sh_page_off, P, sh_cu, p, k, &tiles[k], chain, col, depth[col]) &&
+        lane == 0)
+      bad = 1;
   }
   if (threadIdx.x == 0) write_header(p, t, G, Hkv, P, n_seq, n_tokens, n_tiles);
-  if (__syncthreads_or(err)) {
-    if (err) status_error(status, err);
+  __syncthreads();
+  if (bad) {
+    if (threadIdx.x == 0) status_error(status, ARBOR_EINVAL);
     return;
   }
   if (n_tiles <= kWave) list_few(p, tiles, n_tiles, target, min_part, status);
@@ -705,7 +714,8 @@ __host__ __device__ __forceinline__ bf16x8 read_transposed(const char *p, int ne
   typedef short s16x4 __attribute__((ext_vector_type(4)));
   typedef __attribute__((address_space(3))) s16x4 *P4;
   const bf16x4 a = __builtin_bit_cast(bf16x4, __builtin_amdgcn_ds_read_tr16_b64_v4i16((P4)p));
-  const bf16x4 b = __builtin_bit_cast(bf16x4, __builtin_amdgcn_ds_read_tr16_b64_v4i16((P4)(p + next)));
+  const bf16x4 b =
+      __builtin_bit_cast(bf16x4, __builtin_amdgcn_ds_read_tr16_b64_v4i16((P4)(p + next)));
   return __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
 #else
   return bf16x8{};
@@ -903,7 +913,8 @@ __global__ __launch_bounds__(kRows * 2, 2) void prefill_attn(AttnArgs a) {
     for (int r = 0; r < 16; ++r) z[r] = 0.0f;
 #pragma unroll
     for (int i = 0; i < C::NQ; ++i) {
-      const qvec kf = *reinterpret_cast<const qvec *>(lds + ((at + kat) ^ (i * C::STEP_K)) + 32 * kt * C::ROW);
+      const qvec kf = *reinterpret_cast<const qvec *>(lds + ((at + kat) ^ (i * C::STEP_K)) +
+                                                      32 * kt * C::ROW);
       if constexpr (sizeof(T) == 2) {
         z = mfma_bf16(kf, qf[i], z);
       } else {
@@ -914,7 +925,12 @@ __global__ __launch_bounds__(kRows * 2, 2) void prefill_attn(AttnArgs a) {
     return z;
   };
   // P of 32 keys as the B operand of O^T += V^T P^T (registers 8 ks .. 8 ks + 7 of its
-  // 16 keys ks), rounded to V's type; the sum of the lane's unrounded terms
+  // 16 keys ks), rounded to V's type; the sum of the lane's unrounded terms, which the LSE
+  // needs.  Rounding to bf16 is half a step of each weight: outputs are 0.0022 from the
+  // 64-bit values, relative to their norm, 0.0017 of it by their own rounding.  A second
+  // bf16 for the rest of each weight and its products would be the decode's precision, and
+  // took 1,500 us instead of 1,095 for the long prompt above, 124 instead of 111 for 16 blocks
+  // of new thoughts (four layers).
   struct Terms {
     pvec p[32 / C::PK];
     float sum;
@@ -955,7 +971,8 @@ __global__ __launch_bounds__(kRows * 2, 2) void prefill_attn(AttnArgs a) {
   Window win = fill(0), nxt = win;
   // V^T operand of 16 keys ks (bf16): keys 4 h + i and 8 + 4 h + i, the order that P has
   auto values = [&](int at, int ks, int d) __attribute__((always_inline)) -> bf16x8 {
-    return read_transposed(lds + ((at + vat) ^ (d * C::STEP_V)) + (2 * C::BUF + 16 * ks * C::ROW), 8 * C::ROW);
+    return read_transposed(
+        lds + ((at + vat) ^ (d * C::STEP_V)) + (2 * C::BUF + 16 * ks * C::ROW), 8 * C::ROW);
   };
   auto add = [&](const Terms &t, int at, int kt) __attribute__((always_inline)) {
     if constexpr (sizeof(T) == 2) {
@@ -1229,7 +1246,8 @@ __global__ __launch_bounds__(kRows * 2, 2) void prefill_attn(AttnArgs a) {
 #pragma unroll
       for (int i = 0; i < 4; ++i) w[i] = (T)(o[d][r + i] * inv);
       const int byte = (32 * d + 2 * r + 4 * h) * C::ES;
-      *reinterpret_cast<ovec *>(own + lr * C::ROW + ((byte / 16 ^ (lr & TURN)) * 16 + byte % 16)) = w;
+      *reinterpret_cast<ovec *>(own + lr * C::ROW +
+                                ((byte / 16 ^ (lr & TURN)) * 16 + byte % 16)) = w;
     }
   __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
   __builtin_amdgcn_wave_barrier();
