@@ -394,7 +394,8 @@ int arbor_prefill_plan(const arbor_geom_t *geom, const arbor_tree_t *tree, const
   ARBOR_TRY(check_prefill(geom, n_seq, n_tokens));
   ARBOR_TRY(check_tree(tree));
   if (!status || !plan || reinterpret_cast<uintptr_t>(plan) % 256 != 0) return ARBOR_EINVAL;
-  if (n_tokens > 0 && n_seq > 0 && (!nodes || !cu)) return ARBOR_EINVAL;
+  // (a tree without blocks has none that a token could belong to, nor any arrays)
+  if (n_tokens > 0 && n_seq > 0 && (!nodes || !cu || tree->num_nodes == 0)) return ARBOR_EINVAL;
   return launch_prefill_plan(geom, tree, nodes, n_seq, cu, n_tokens, plan, plan_bytes, status,
                              stream);
 }
@@ -409,7 +410,8 @@ int arbor_tree_prefill_attn(const arbor_geom_t *geom, const arbor_tree_t *tree,
   ARBOR_TRY(check_pool(pool));
   if (!status || !plan || reinterpret_cast<uintptr_t>(plan) % 256 != 0) return ARBOR_EINVAL;
   if (layer < 0 || layer >= geom->num_layers) return ARBOR_EINVAL;
-  if (n_tokens > 0 && n_seq > 0 && (!q || !out || !workspace)) return ARBOR_EINVAL;
+  if (n_tokens > 0 && n_seq > 0 && (!q || !out || !workspace || tree->num_nodes == 0))
+    return ARBOR_EINVAL;
   const void *ptrs[] = {q, out, pool->k, pool->v, workspace};
   for (const void *p : ptrs)
     if (reinterpret_cast<uintptr_t>(p) % 16 != 0) return ARBOR_EUNSUPPORTED;
